@@ -340,6 +340,145 @@ int tac_calibrate(const uint16_t* Z_fp, const uint16_t* Z_q, int32_t N, int32_t 
                   uint16_t* tac_M, uint16_t* tac_d, double* M64, double* d64,
                   void* ws, size_t ws_bytes, void* stream);
 
+/*
+ * Rotary positions.  Pair j of the first `rot` entries of a head turns by the
+ * angle pos freq[j]: (u, v) -> amplitude (u cos - v sin, v cos + u sin), in fp32
+ * with one rounding to fp16; the angle is formed and reduced to a turn in fp64, so
+ * far positions keep their precision.  Entries from rot on are copied.
+ *   layout    SQ_ROPE_HALF: pair j is entries (j, j + rot / 2); SQ_ROPE_PAIRS:
+ *             entries (2 j, 2 j + 1).
+ *   transpose non-zero: the sine's sign is flipped, which is the transposed map:
+ *             the gradient, and with amplitude 1 the inverse.
+ *   X  [T][H][D] fp16; x_token and x_head are its strides in elements between
+ *      tokens and heads, multiples of 8 (a view into a fused projection's rows);
+ *      Y likewise.  Y may be X with the same strides; other overlaps are not
+ *      allowed.
+ *   pos  [T] int32 positions, any sign; NULL: the token's index.
+ *   freq [rot / 2] fp64, radians per position: sq_rope_frequencies or one's own.
+ *   D % 16 == 0, 16 <= D <= 1024; rot even, 2 <= rot <= D; T H D < 2^35.
+ *
+ * sq_rope_frequencies fills freq with base^(-2 j / rot), scaled for contexts
+ * `factor` >= 1 times the original:
+ *   SQ_ROPE_NONE    as they are (factor is ignored).
+ *   SQ_ROPE_LINEAR  divided by factor.
+ *   SQ_ROPE_NTK     base times factor^(rot / (rot - 2)): pair 0 as it is, the last
+ *                   divided by factor.
+ *   SQ_ROPE_YARN    a pair that makes beta_fast turns or more over the original
+ *                   context (`original` tokens) as it is, one that makes beta_slow
+ *                   or fewer divided by factor, linear in the turns between (the
+ *                   YaRN paper's 32 and 1); beta_fast > beta_slow >= 0.
+ * sq_rope_amplitude: what YaRN scales cos and sin by, 0.1 ln(factor) + 1; 1 for
+ * the others.
+ */
+#define SQ_ROPE_HALF 0
+#define SQ_ROPE_PAIRS 1
+#define SQ_ROPE_NONE 0
+#define SQ_ROPE_LINEAR 1
+#define SQ_ROPE_NTK 2
+#define SQ_ROPE_YARN 3
+int sq_rope_frequencies(int32_t rot, double base, int32_t scaling, double factor, double original, double beta_fast,
+                        double beta_slow, double* freq, void* stream);
+double sq_rope_amplitude(int32_t scaling, double factor);
+int sq_rope(const uint16_t* X, int64_t x_token, int64_t x_head, const int32_t* pos, const double* freq, int32_t T,
+            int32_t H, int32_t D, int32_t rot, int32_t layout, int32_t transpose, float amplitude, uint16_t* Y,
+            int64_t y_token, int64_t y_head, void* stream);
+
+/*
+ * A paged key / value cache in 8 bits, one fp32 scale for each page and head (the
+ * quantiser of sgat_quantize_w8: s = absmax / 127, codes clamp(rint(x / s), -128,
+ * 127), zero codes for a zero scale).
+ *   k        [pages][heads][page][dim] int8     v        [pages][heads][dim][page] int8
+ *   k_scale  [pages][heads] fp32                v_scale  [pages][heads] fp32
+ * `page` tokens a page: 16, 32, 64 or 128; dim % 16 == 0, 16 <= dim <= 256; heads
+ * are the key heads, 1 .. 1024.  Values are stored channel by channel so that the
+ * attention reads both as matrix operands.
+ *
+ * A batch of B sequences, ragged:
+ *   cu     [B + 1] int32, non-decreasing: sequence b's new tokens are rows cu[b] ..
+ *          cu[b + 1] - 1 of the batch's T rows (none is allowed).  Rows of no
+ *          sequence are neither read nor written.
+ *   lens   [B] int32: positions of sequence b in the cache, its new tokens being
+ *          the last of them, so that its i-th new token has position
+ *          lens[b] - (cu[b + 1] - cu[b]) + i.
+ *   table  [B][max_pages] int32: position p lies in page table[b][p / page], slot
+ *          p % page.  An entry outside 0 .. pages - 1 is no page: what would be
+ *          written there is dropped, and its keys are masked.  Entries past the
+ *          length are not read.
+ * The three live on the device, where no check of them is possible before a launch:
+ * rows are clamped to 0 .. T and lengths to 0 .. max_pages page, so no value of them
+ * reads or writes outside the tensors.  max_pages page <= 2^28, T <= 2^24.
+ *
+ * kv_append writes the new tokens' keys, rotated if freq is given (rotation as
+ * sq_rope's, quantised from fp32), and values into the pages, and, if Q is given,
+ * the rotated queries into Qr.
+ *   A page whose slot 0 is written takes its scale from the new tokens; another
+ *   keeps max(its scale, theirs), and where that grows its older codes become
+ *   rint(code s_old / s_new).  Calling it again with the same arguments changes
+ *   nothing.  Codes of slots from the length on keep their bytes.  New tokens
+ *   before position 0 (a length shorter than their number) are dropped.  No two
+ *   sequences of a call may write the same page.
+ *   K, V [T][heads][dim] and Q, Qr [T][Hq][dim] fp16 with strides as in sq_rope;
+ *   Qr may be Q with the same strides.
+ *   pos  [T] int32 rotary positions; NULL: the cache positions.
+ *   (T / page + 2 B) heads + T Hq dim / 4096 < 2^24.
+ * kv_read: the listed pages as values code scale, rounded to fp16: K and V
+ *   [n][heads][page][dim]; zeros for an entry that is no page.  n heads < 2^24.
+ */
+typedef struct sq_kv_cache {
+    int8_t* k;
+    int8_t* v;
+    float* k_scale;
+    float* v_scale;
+    int32_t pages, page, heads, dim;
+} sq_kv_cache;
+int kv_append(const sq_kv_cache* cache, const uint16_t* K, int64_t k_token, int64_t k_head, const uint16_t* V,
+              int64_t v_token, int64_t v_head, const int32_t* cu, const int32_t* lens, const int32_t* table, int32_t T,
+              int32_t B, int32_t max_pages, const int32_t* pos, const double* freq, int32_t rot, int32_t layout,
+              float amplitude, const uint16_t* Q, int64_t q_token, int64_t q_head, int32_t Hq, uint16_t* Qr,
+              int64_t r_token, int64_t r_head, void* stream);
+int kv_read(const sq_kv_cache* cache, const int32_t* list, int32_t n, uint16_t* K, uint16_t* V, void* stream);
+
+/*
+ * attn_kv8 -- attention of the new tokens' queries over the cache (after
+ * kv_append): O = softmax(scale q . k) v over the visible keys, query head h reading
+ * key head h / (Hq / heads); Hq is a multiple of heads, at most 1024.
+ *   A query at position p sees the positions 0 .. lens[b] - 1 of its sequence, with
+ *   causal non-zero those up to p, with window > 0 those from p - window + 1 on.  A
+ *   row that sees no key gives zeros, and lse -inf.
+ *   Arithmetic: products of q with the codes summed in fp32 on the fp16 matrix
+ *   cores, scales and softmax in fp32; the softmax weights times their value scale
+ *   are rounded to fp16 (2^-11 relative) for the second product, summed in fp32, and
+ *   the result is rounded once to fp16.
+ *   Q    [T][Hq][dim] fp16, strides as in sq_rope.   O out [T][Hq][dim] fp16, dense.
+ *   lse  out [T][Hq] fp32, the natural logarithm of the softmax's sum, or NULL.
+ *   ws   device workspace of at least sq_attn_kv8_workspace_bytes() for the same
+ *        sizes, max_len = max_pages page.  Its contents need no preparation; two
+ *        calls that may run at the same time need one each.
+ */
+size_t sq_attn_kv8_workspace_bytes(int32_t T, int32_t B, int32_t Hq, int32_t heads, int32_t dim, int32_t max_len);
+int attn_kv8(const uint16_t* Q, int64_t q_token, int64_t q_head, const sq_kv_cache* cache, const int32_t* cu,
+             const int32_t* lens, const int32_t* table, int32_t T, int32_t B, int32_t max_pages, int32_t Hq,
+             int32_t causal, int32_t window, float scale, uint16_t* O, float* lse, void* ws, size_t ws_bytes,
+             void* stream);
+
+/*
+ * Weight-only 4-bit products: fp16 activations, int4 weights with one fp16 scale
+ * for each output channel and group of `group` inputs, for linears whose
+ * activations stay unquantised at decode.
+ *   sq_quantize_weights_group: per group s = fp16(absmax / 7), codes
+ *     clamp(rint(w / s), -8, 7) against the rounded s (zero codes for s = 0).
+ *     W [N][K] fp16 in; Wq [N][K/2] packed int4 out, s_w [K / group][N] fp16 out.
+ *   w4a16_gemm_frag: Y[m][n] = fp16(sum_G s_w[G][n] sum_{k in G} X[m][k] q[n][k]),
+ *     sums in fp32, each group's scale applied to its fp32 sum.  X [M][K] fp16, Wf
+ *     from sq_weights_to_frag, Y out [M][N] fp16.  Any M; made for few rows, past
+ *     which w4a4_gemm_frag on quantised activations is the faster product.
+ *   group: 32, 64 or a multiple of 128, dividing K.  N % 8 == 0.
+ */
+int sq_quantize_weights_group(const uint16_t* W, int32_t N, int32_t K, int32_t group, uint8_t* Wq, uint16_t* s_w,
+                              void* stream);
+int w4a16_gemm_frag(const uint16_t* X, const uint8_t* Wf, const uint16_t* s_w, int32_t M, int32_t N, int32_t K,
+                    int32_t group, uint16_t* Y, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -9,15 +9,23 @@ and streams.  Outputs and workspaces are allocated with torch when not given.
     Wq, s_w = sgat_prepare_weights(W, P)             # Eq. 12, offline
     Y = w4a4_gemm(Aq, s_a, Wq, s_w)                  # Eq. 13
     Zc = tac_apply(Z, tac_M, tac_d, g)               # Eq. 17
+
+Between the projections, attention over a paged 8-bit cache:
+
+    cache = kv_cache(pages, heads, dim)
+    freq = rope_frequencies(dim, 1e6)
+    q = kv_append(cache, k, v, cu, lens, table, freq=freq, q=q)
+    Z = attn_kv8(q, cache, cu, lens, table)
 """
 from __future__ import annotations
 
 import functools
-from typing import Optional, Tuple
+import math
+from typing import NamedTuple, Optional, Tuple
 
 import torch
 
-from ._lib import SQ_OK, StarQuantError, check, lib  # noqa: F401
+from ._lib import KVCacheStruct, SQ_OK, StarQuantError, check, lib  # noqa: F401
 
 __all__ = ["sgat_prepare_weights", "sgat_transform", "sgat_quantize", "sgat_quant_act", "w4a4_gemm", "tac_apply",
            "tac_default_block", "default_band", "quant_act_workspace_bytes", "gemm_workspace_bytes",
@@ -25,7 +33,9 @@ __all__ = ["sgat_prepare_weights", "sgat_transform", "sgat_quantize", "sgat_quan
            "sgat_prepare_weights_w8", "sgat_quantize_w8", "sgat_quant_act_w8", "w8a8_gemm",
            "tac_calibrate", "tac_calibrate_workspace_bytes", "sgat_split_basis", "sgat_transform_fast",
            "fp6_row_bytes", "codes_to_fp6", "w4a4_gemm_fp6",
-           "frag_weight_bytes", "weights_to_frag", "w4a4_gemm_frag", "w8a8_gemm_frag"]
+           "frag_weight_bytes", "weights_to_frag", "w4a4_gemm_frag", "w8a8_gemm_frag",
+           "rope_frequencies", "rope_amplitude", "rope", "KVCache", "kv_cache", "kv_append", "kv_read", "attn_kv8",
+           "attn_kv8_workspace_bytes", "quantize_weights_group", "w4a16_gemm_frag"]
 
 
 def _on_stream(fn):
@@ -428,3 +438,237 @@ def sgat_transform_fast(X: torch.Tensor, state: Optional[torch.Tensor], Ps: torc
     _need(out, "out", torch.float32, (M, K))
     check(lib().sgat_transform_fast(_ptr(X), _ptr(state), _ptr(Ps), M, K, d_m, d_u, _ptr(out), _stream(stream)))
     return out
+
+
+ROPE_LAYOUTS = {"half": 0, "pairs": 1}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
+
+
+def _run(fn, tensors, args, stream):
+    """check(fn(*args, stream)) on the device that the tensors (None: not given) are all on,
+    which need not be the current one."""
+    dev = tensors[0].get_device()
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise ValueError("the tensors are on different devices")
+    current = _device() if _device is not None else torch.cuda.current_device()
+    if dev == current:
+        check(fn(*args, _stream(stream)))
+    elif stream is not None:
+        raise ValueError("the stream is on another device than the tensors")
+    else:
+        with torch.cuda.device(dev):
+            check(fn(*args, _stream(None)))
+
+
+def _choice(table: dict, key, name: str) -> int:
+    if key not in table:
+        raise ValueError(f"{name} must be one of {sorted(table)}, got {key!r}")
+    return table[key]
+
+
+@_on_stream
+def rope_frequencies(rot: int, base: float, *, scaling: str = "none", factor: float = 1.0, original: float = 0.0,
+                     beta_fast: float = 32.0, beta_slow: float = 1.0, device="cuda", out=None, stream=None):
+    """Radians per position of each rotary pair, fp64 [rot / 2]: base^(-2 j / rot), scaled
+    ("linear", "ntk" or "yarn") for contexts `factor` times the `original` length."""
+    kind = _choice(ROPE_SCALINGS, scaling, "scaling")
+    if out is None:
+        out = torch.empty((max(0, rot // 2),), dtype=torch.float64, device=device)
+    _need(out, "out", torch.float64, (rot // 2,))
+    _run(lib().sq_rope_frequencies, (out,), (rot, base, kind, factor, original, beta_fast, beta_slow, _ptr(out)),
+         stream)
+    return out
+
+
+def rope_amplitude(scaling: str, factor: float) -> float:
+    """What a scaling multiplies cos and sin by: 0.1 ln(factor) + 1 for "yarn", else 1."""
+    return float(lib().sq_rope_amplitude(_choice(ROPE_SCALINGS, scaling, "scaling"), factor))
+
+
+def _heads(t: torch.Tensor, name: str, shape=None):
+    """Checks a [T, H, D] fp16 device tensor, dense in D; returns its (token, head) strides."""
+    if t is None:
+        raise ValueError(f"{name} is required")
+    if not t.is_cuda or t.dtype is not torch.float16:
+        raise ValueError(f"{name} must be a torch.float16 device tensor")
+    if t.dim() != 3 or (shape is not None and t.shape != shape):
+        raise ValueError(f"{name} must have shape {tuple(shape) if shape else '[T, H, D]'}, got {tuple(t.shape)}")
+    s = t.stride()
+    if s[2] != 1:
+        raise ValueError(f"{name} must be dense in its last dimension")
+    return s[0], s[1]
+
+
+@_on_stream
+def rope(X: torch.Tensor, freq: torch.Tensor, pos: Optional[torch.Tensor] = None, *, layout: str = "half",
+         amplitude: float = 1.0, transpose: bool = False, out=None, stream=None):
+    """Rotary positions on [T, H, D] heads (any strides of T and H that are multiples of 8):
+    the first 2 len(freq) entries of each head turn by pos freq (pos [T] int32, default the
+    token's index).  transpose=True applies the transposed map (the gradient).  out may be X."""
+    T, H, D = X.shape
+    xs = _heads(X, "X")
+    _need(freq, "freq", torch.float64, (freq.numel(),))
+    _need(pos, "pos", torch.int32, (T,), optional=True)
+    if out is None:
+        out = torch.empty((T, H, D), dtype=torch.float16, device=X.device)
+    ys = _heads(out, "out", (T, H, D))
+    _run(lib().sq_rope, (X, freq, pos, out),
+         (_ptr(X), *xs, _ptr(pos), _ptr(freq), T, H, D, 2 * freq.numel(), _choice(ROPE_LAYOUTS, layout, "layout"),
+          int(transpose), amplitude, _ptr(out), *ys), stream)
+    return out
+
+
+class KVCache(NamedTuple):
+    """A paged 8-bit key / value cache: codes k [pages, heads, page, dim] and
+    v [pages, heads, dim, page], fp32 scales [pages, heads]."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: torch.Tensor
+    v_scale: torch.Tensor
+
+    def struct(self) -> KVCacheStruct:
+        """The sq_kv_cache of this cache, its tensors checked."""
+        if self.k.dim() != 4:
+            raise ValueError(f"k must have shape [pages, heads, page, dim], got {tuple(self.k.shape)}")
+        pages, heads, page, dim = self.k.shape
+        _need(self.k, "k", torch.int8)
+        _need(self.v, "v", torch.int8, (pages, heads, dim, page))
+        _need(self.k_scale, "k_scale", torch.float32, (pages, heads))
+        _need(self.v_scale, "v_scale", torch.float32, (pages, heads))
+        return KVCacheStruct(self.k.data_ptr(), self.v.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr(),
+                             pages, page, heads, dim)
+
+
+def kv_cache(pages: int, heads: int, dim: int, page: int = 64, device="cuda") -> KVCache:
+    """An empty cache of `pages` pages of `page` tokens (zero codes and scales)."""
+    return KVCache(torch.zeros((pages, heads, page, dim), dtype=torch.int8, device=device),
+                   torch.zeros((pages, heads, dim, page), dtype=torch.int8, device=device),
+                   torch.zeros((pages, heads), dtype=torch.float32, device=device),
+                   torch.zeros((pages, heads), dtype=torch.float32, device=device))
+
+
+def _batch(cu, lens, table):
+    if lens is None or table is None or table.dim() != 2:
+        raise ValueError("lens [B] and table [B, max_pages] are required")
+    B, max_pages = table.shape
+    _need(cu, "cu", torch.int32, (B + 1,))
+    _need(lens, "lens", torch.int32, (B,))
+    _need(table, "table", torch.int32)
+    return B, max_pages
+
+
+@_on_stream
+def kv_append(cache: KVCache, K: torch.Tensor, V: torch.Tensor, cu: torch.Tensor, lens: torch.Tensor,
+              table: torch.Tensor, *, freq: Optional[torch.Tensor] = None, pos: Optional[torch.Tensor] = None,
+              layout: str = "half", amplitude: float = 1.0, q: Optional[torch.Tensor] = None, q_out=None, stream=None):
+    """New tokens' keys (rotated when freq is given) and values [T, heads, dim] into the cache.
+    Sequence b's tokens are rows cu[b] .. cu[b + 1] - 1 and the last of its lens[b] positions;
+    position p lies in page table[b, p // page].  With q [T, Hq, dim] the queries are rotated
+    too and returned (q_out may be q)."""
+    c = cache.struct()
+    B, max_pages = _batch(cu, lens, table)
+    T = K.shape[0]
+    ks = _heads(K, "K", (T, c.heads, c.dim))
+    vs = _heads(V, "V", (T, c.heads, c.dim))
+    _need(freq, "freq", torch.float64, None if freq is None else (freq.numel(),), optional=True)
+    _need(pos, "pos", torch.int32, (T,), optional=True)
+    qs = rs = (0, 0)
+    Hq = 0
+    if q is not None:
+        if freq is None:
+            raise ValueError("q needs freq")
+        Hq = q.shape[1]
+        qs = _heads(q, "q", (T, Hq, c.dim))
+        if q_out is None:
+            q_out = torch.empty((T, Hq, c.dim), dtype=torch.float16, device=q.device)
+        rs = _heads(q_out, "q_out", (T, Hq, c.dim))
+    else:
+        q_out = None
+    _run(lib().kv_append, (*cache, K, V, cu, lens, table, pos, freq, q, q_out),
+         (c, _ptr(K), *ks, _ptr(V), *vs, _ptr(cu), _ptr(lens), _ptr(table), T, B, max_pages, _ptr(pos), _ptr(freq),
+          0 if freq is None else 2 * freq.numel(), _choice(ROPE_LAYOUTS, layout, "layout"), amplitude, _ptr(q), *qs, Hq,
+          _ptr(q_out), *rs), stream)
+    return q_out
+
+
+@_on_stream
+def kv_read(cache: KVCache, pages: torch.Tensor, *, K=None, V=None, stream=None):
+    """The listed pages (int32 [n]) as the values they hold: fp16 K and V [n, heads, page, dim]."""
+    c = cache.struct()
+    _need(pages, "pages", torch.int32, (pages.numel(),))
+    shape = (pages.numel(), c.heads, c.page, c.dim)
+    if K is None:
+        K = torch.empty(shape, dtype=torch.float16, device=pages.device)
+    if V is None:
+        V = torch.empty(shape, dtype=torch.float16, device=pages.device)
+    _need(K, "K", torch.float16, shape)
+    _need(V, "V", torch.float16, shape)
+    _run(lib().kv_read, (*cache, pages, K, V), (c, _ptr(pages), shape[0], _ptr(K), _ptr(V)), stream)
+    return K, V
+
+
+def attn_kv8_workspace_bytes(T: int, B: int, Hq: int, heads: int, dim: int, max_len: int) -> int:
+    return int(lib().sq_attn_kv8_workspace_bytes(T, B, Hq, heads, dim, max_len))
+
+
+@_on_stream
+def attn_kv8(q: torch.Tensor, cache: KVCache, cu: torch.Tensor, lens: torch.Tensor, table: torch.Tensor, *,
+             causal: bool = True, window: int = 0, scale: Optional[float] = None, out=None, lse=None,
+             want_lse: bool = False, ws=None, stream=None):
+    """Attention of the queries [T, Hq, dim] over the cache; batch arguments as in kv_append,
+    after which it is called.  scale defaults to dim^-0.5.  A row that sees no key gives zeros
+    (lse -inf); rows of no sequence are left as they were.  Returns out [T, Hq, dim], or
+    (out, lse [T, Hq] fp32)."""
+    c = cache.struct()
+    B, max_pages = _batch(cu, lens, table)
+    T, Hq = q.shape[:2]
+    qs = _heads(q, "q", (T, Hq, c.dim))
+    if out is None:
+        out = torch.empty((T, Hq, c.dim), dtype=torch.float16, device=q.device)
+    if lse is None and want_lse:
+        lse = torch.empty((T, Hq), dtype=torch.float32, device=q.device)
+    _need(out, "out", torch.float16, (T, Hq, c.dim))
+    _need(lse, "lse", torch.float32, (T, Hq), optional=True)
+    ws, wsb = _ws(attn_kv8_workspace_bytes(T, B, Hq, c.heads, c.dim, max_pages * c.page), ws, q.device)
+    _run(lib().attn_kv8, (q, *cache, cu, lens, table, out, lse, ws),
+         (_ptr(q), *qs, c, _ptr(cu), _ptr(lens), _ptr(table), T, B, max_pages, Hq, int(causal), window,
+          1.0 / math.sqrt(c.dim) if scale is None else scale, _ptr(out), _ptr(lse), _ptr(ws), wsb), stream)
+    return (out, lse) if want_lse or lse is not None else out
+
+
+@_on_stream
+def quantize_weights_group(W: torch.Tensor, group: int = 128, *, Wq=None, s_w=None, stream=None):
+    """fp16 weights [N, K] -> packed int4 codes [N, K/2] and fp16 scales [K/group, N], one for
+    each output channel and group of inputs."""
+    N, K = W.shape
+    _need(W, "W", torch.float16)
+    if group < 1 or K % group:
+        raise ValueError(f"group={group} must divide K={K}")
+    if Wq is None:
+        Wq = torch.empty((N, K // 2), dtype=torch.uint8, device=W.device)
+    if s_w is None:
+        s_w = torch.empty((K // group, N), dtype=torch.float16, device=W.device)
+    _need(Wq, "Wq", torch.uint8, (N, K // 2))
+    _need(s_w, "s_w", torch.float16, (K // group, N))
+    _run(lib().sq_quantize_weights_group, (W, Wq, s_w), (_ptr(W), N, K, group, _ptr(Wq), _ptr(s_w)), stream)
+    return Wq, s_w
+
+
+@_on_stream
+def w4a16_gemm_frag(X: torch.Tensor, Wf: torch.Tensor, s_w: torch.Tensor, *, Y=None, stream=None):
+    """Y = X W^T for fp16 rows X [M, K] and 4-bit weights with group scales: Wf the codes in
+    fragment order (weights_to_frag), s_w [K/group, N] fp16 (quantize_weights_group).  Made for
+    few rows."""
+    M, K = X.shape
+    ng, N = s_w.shape
+    if ng < 1 or K % ng:
+        raise ValueError(f"s_w has {ng} groups, which do not divide K={K}")
+    _need(X, "X", torch.float16)
+    _need(Wf, "Wf", torch.uint8, _frag_shape(N, K, 4))
+    _need(s_w, "s_w", torch.float16, (ng, N))
+    if Y is None:
+        Y = torch.empty((M, N), dtype=torch.float16, device=X.device)
+    _need(Y, "Y", torch.float16, (M, N))
+    _run(lib().w4a16_gemm_frag, (X, Wf, s_w, Y), (_ptr(X), _ptr(Wf), _ptr(s_w), M, N, K, K // ng, _ptr(Y)), stream)
+    return Y

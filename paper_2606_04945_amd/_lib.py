@@ -12,6 +12,16 @@ SQ_OK, SQ_ERR_NULL, SQ_ERR_SHAPE, SQ_ERR_ALIGN, SQ_ERR_WORKSPACE, SQ_ERR_HIP = r
 
 # name -> (restype, argtypes); mirrors include/starquant.h
 _p, _i32, _sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t
+_i64, _f32, _f64 = ctypes.c_int64, ctypes.c_float, ctypes.c_double
+
+
+class KVCacheStruct(ctypes.Structure):
+    """sq_kv_cache."""
+    _fields_ = [("k", _p), ("v", _p), ("k_scale", _p), ("v_scale", _p),
+                ("pages", _i32), ("page", _i32), ("heads", _i32), ("dim", _i32)]
+
+
+_cache = ctypes.POINTER(KVCacheStruct)
 SIGNATURES = {
     "sq_last_error": (ctypes.c_char_p, []),
     "sq_version": (ctypes.c_char_p, []),
@@ -45,6 +55,17 @@ SIGNATURES = {
     "sq_tac_calibrate_workspace_bytes": (_sz, [_i32, _i32, _i32]),
     "tac_calibrate": (ctypes.c_int, [_p, _p, _i32, _i32, _i32, ctypes.c_double, ctypes.c_double, ctypes.c_double,
                                      ctypes.c_double, _p, _p, _p, _p, _p, _sz, _p]),
+    "sq_rope_frequencies": (ctypes.c_int, [_i32, _f64, _i32, _f64, _f64, _f64, _f64, _p, _p]),
+    "sq_rope_amplitude": (_f64, [_i32, _f64]),
+    "sq_rope": (ctypes.c_int, [_p, _i64, _i64, _p, _p, _i32, _i32, _i32, _i32, _i32, _i32, _f32, _p, _i64, _i64, _p]),
+    "kv_append": (ctypes.c_int, [_cache, _p, _i64, _i64, _p, _i64, _i64, _p, _p, _p, _i32, _i32, _i32, _p, _p, _i32,
+                                 _i32, _f32, _p, _i64, _i64, _i32, _p, _i64, _i64, _p]),
+    "kv_read": (ctypes.c_int, [_cache, _p, _i32, _p, _p, _p]),
+    "sq_attn_kv8_workspace_bytes": (_sz, [_i32, _i32, _i32, _i32, _i32, _i32]),
+    "attn_kv8": (ctypes.c_int, [_p, _i64, _i64, _cache, _p, _p, _p, _i32, _i32, _i32, _i32, _i32, _i32, _f32, _p, _p,
+                                _p, _sz, _p]),
+    "sq_quantize_weights_group": (ctypes.c_int, [_p, _i32, _i32, _i32, _p, _p, _p]),
+    "w4a16_gemm_frag": (ctypes.c_int, [_p, _p, _p, _i32, _i32, _i32, _i32, _p, _p]),
 }
 
 

@@ -5,6 +5,8 @@
 #include <stdlib.h>
 #include <stdio.h>
 
+#include <math.h>
+
 #include <atomic>
 #include <mutex>
 
@@ -513,6 +515,229 @@ int sgat_transform_fast(const uint16_t* X, const uint8_t* state, const uint16_t*
                "sgat_transform_fast: X, Ps and Xp must be 16-byte aligned");
     return hip_status(sq::launch_transform_fast(X, state, Ps, M, K, d_m, d_u, Xp, static_cast<hipStream_t>(stream)),
                       "transform_fast");
+}
+
+}  // extern "C"
+
+// ---- rotary positions, the paged 8-bit cache, attention over it, weight-only products ----
+
+namespace {
+
+bool aligned4(const void* p) { return ((uintptr_t)p & 3u) == 0; }
+
+constexpr int32_t kMaxTokens = 1 << 24, kMaxPositions = 1 << 28;
+constexpr int64_t kMaxBlocks = 1 << 24;      // workgroups of 256 threads that one launch's grid holds
+
+// Strides of a [T][H][D] tensor, dense in D; those of an extent of one do not count.
+int check_strides(int64_t token, int64_t head, int32_t T, int32_t H, int32_t D, bool out, const char* name,
+                  const char* what) {
+    const int64_t t = T > 1 ? token : 0, h = H > 1 ? head : 0;
+    if (t < 0 || h < 0 || t % 8 || h % 8 || t > ((int64_t)1 << 40) || h > ((int64_t)1 << 40))
+        return fail(SQ_ERR_SHAPE, "%s: strides of %s (%lld, %lld): need multiples of 8, not negative", name, what,
+                    (long long)token, (long long)head);
+    const bool apart = (T == 1 && H == 1) || (T == 1 && h >= D) || (H == 1 && t >= D) ||
+                       (h >= D && t >= (H - 1) * h + D) || (t >= D && h >= (T - 1) * t + D);
+    if (out && !apart)
+        return fail(SQ_ERR_SHAPE, "%s: strides of %s (%lld, %lld): its rows overlap", name, what, (long long)token,
+                    (long long)head);
+    return SQ_OK;
+}
+
+int check_rotation(int32_t rot, int32_t layout, float amplitude, int32_t D, const char* name) {
+    SQ_REQUIRE(rot >= 2 && rot <= D && rot % 2 == 0, SQ_ERR_SHAPE, "%s: rot=%d: need an even 2 .. %d", name, rot, D);
+    SQ_REQUIRE(layout == SQ_ROPE_HALF || layout == SQ_ROPE_PAIRS, SQ_ERR_SHAPE, "%s: layout=%d", name, layout);
+    SQ_REQUIRE(isfinite(amplitude), SQ_ERR_SHAPE, "%s: the amplitude is not finite", name);
+    return SQ_OK;
+}
+
+int check_cache(const sq_kv_cache* c, const char* name) {
+    SQ_REQUIRE(c, SQ_ERR_NULL, "%s: cache is required", name);
+    SQ_REQUIRE(c->page == 16 || c->page == 32 || c->page == 64 || c->page == 128, SQ_ERR_SHAPE,
+               "%s: page=%d: need 16, 32, 64 or 128 tokens", name, c->page);
+    SQ_REQUIRE(c->dim >= 16 && c->dim <= 256 && c->dim % 16 == 0, SQ_ERR_SHAPE,
+               "%s: dim=%d: need a multiple of 16 in 16 .. 256", name, c->dim);
+    SQ_REQUIRE(c->heads >= 1 && c->heads <= 1024, SQ_ERR_SHAPE, "%s: heads=%d: need 1 .. 1024", name, c->heads);
+    SQ_REQUIRE(c->pages >= 1, SQ_ERR_SHAPE, "%s: pages=%d: need at least one", name, c->pages);
+    SQ_REQUIRE(c->k && c->v && c->k_scale && c->v_scale, SQ_ERR_NULL, "%s: the cache's four tensors are required",
+               name);
+    SQ_REQUIRE(aligned16(c->k) && aligned16(c->v) && aligned16(c->k_scale) && aligned16(c->v_scale), SQ_ERR_ALIGN,
+               "%s: pointers must be 16-byte aligned", name);
+    return SQ_OK;
+}
+
+int check_batch(const sq_kv_cache* c, const int32_t* cu, const int32_t* lens, const int32_t* table, int32_t T,
+                int32_t B, int32_t max_pages, const char* name) {
+    SQ_REQUIRE(T >= 0 && T <= kMaxTokens && B >= 0, SQ_ERR_SHAPE, "%s: T=%d B=%d: need 0 <= T <= %d, B >= 0", name, T,
+               B, kMaxTokens);
+    SQ_REQUIRE(max_pages >= 0 && (int64_t)max_pages * c->page <= kMaxPositions, SQ_ERR_SHAPE,
+               "%s: max_pages=%d: need at most %d positions", name, max_pages, kMaxPositions);
+    if (T == 0 || B == 0) return SQ_OK;
+    SQ_REQUIRE(cu && lens && (table || max_pages == 0), SQ_ERR_NULL, "%s: cu, lens and table are required", name);
+    SQ_REQUIRE(aligned4(cu) && aligned4(lens) && aligned4(table), SQ_ERR_ALIGN,
+               "%s: cu, lens and table must be 4-byte aligned", name);
+    return SQ_OK;
+}
+
+int check_group(int32_t N, int32_t K, int32_t group, const char* name) {
+    SQ_TRY(check_K(K));
+    SQ_REQUIRE((group == 32 || group == 64 || (group > 0 && group % 128 == 0)) && K % group == 0, SQ_ERR_SHAPE,
+               "%s: group=%d: need 32, 64 or a multiple of 128, dividing K=%d", name, group, K);
+    SQ_REQUIRE(N >= 0 && N % 8 == 0, SQ_ERR_SHAPE, "%s: N=%d: need N %% 8 == 0", name, N);
+    return SQ_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int sq_rope_frequencies(int32_t rot, double base, int32_t scaling, double factor, double original, double beta_fast,
+                        double beta_slow, double* freq, void* stream) {
+    SQ_REQUIRE(rot >= 2 && rot <= 1024 && rot % 2 == 0, SQ_ERR_SHAPE,
+               "sq_rope_frequencies: rot=%d: need an even 2 .. 1024", rot);
+    SQ_REQUIRE(scaling >= SQ_ROPE_NONE && scaling <= SQ_ROPE_YARN, SQ_ERR_SHAPE, "sq_rope_frequencies: scaling=%d",
+               scaling);
+    SQ_REQUIRE(base > 1.0 && isfinite(base), SQ_ERR_SHAPE, "sq_rope_frequencies: base=%g: need a finite base > 1",
+               base);
+    SQ_REQUIRE(scaling == SQ_ROPE_NONE || (factor >= 1.0 && isfinite(factor)), SQ_ERR_SHAPE,
+               "sq_rope_frequencies: factor=%g: need a finite factor >= 1", factor);
+    SQ_REQUIRE(scaling != SQ_ROPE_YARN || (original > 0 && isfinite(original) && beta_slow >= 0 &&
+                                           beta_fast > beta_slow && isfinite(beta_fast)),
+               SQ_ERR_SHAPE, "sq_rope_frequencies: original=%g beta_fast=%g beta_slow=%g: need original > 0 and "
+               "beta_fast > beta_slow >= 0", original, beta_fast, beta_slow);
+    SQ_REQUIRE(freq, SQ_ERR_NULL, "sq_rope_frequencies: freq is required");
+    SQ_REQUIRE(aligned16(freq), SQ_ERR_ALIGN, "sq_rope_frequencies: freq must be 16-byte aligned");
+    return hip_status(sq::launch_rope_frequencies(rot, base, scaling, factor, original, beta_fast, beta_slow, freq,
+                                                  static_cast<hipStream_t>(stream)),
+                      "rope_frequencies");
+}
+
+double sq_rope_amplitude(int32_t scaling, double factor) {
+    return scaling == SQ_ROPE_YARN && factor > 1.0 ? 0.1 * log(factor) + 1.0 : 1.0;
+}
+
+int sq_rope(const uint16_t* X, int64_t x_token, int64_t x_head, const int32_t* pos, const double* freq, int32_t T,
+            int32_t H, int32_t D, int32_t rot, int32_t layout, int32_t transpose, float amplitude, uint16_t* Y,
+            int64_t y_token, int64_t y_head, void* stream) {
+    SQ_REQUIRE(D >= 16 && D <= 1024 && D % 16 == 0, SQ_ERR_SHAPE, "sq_rope: D=%d: need a multiple of 16 in 16 .. 1024",
+               D);
+    SQ_TRY(check_rotation(rot, layout, amplitude, D, "sq_rope"));
+    SQ_REQUIRE(T >= 0 && H >= 0 && (double)T * H * D < 0x1p35, SQ_ERR_SHAPE, "sq_rope: T=%d H=%d: need T H D < 2^35", T,
+               H);
+    if (T == 0 || H == 0) return SQ_OK;
+    SQ_TRY(check_strides(x_token, x_head, T, H, D, false, "sq_rope", "X"));
+    SQ_TRY(check_strides(y_token, y_head, T, H, D, true, "sq_rope", "Y"));
+    SQ_REQUIRE(X && Y && freq, SQ_ERR_NULL, "sq_rope: X, Y and freq are required");
+    SQ_REQUIRE(aligned16(X) && aligned16(Y) && aligned16(freq) && aligned4(pos), SQ_ERR_ALIGN,
+               "sq_rope: X, Y and freq must be 16-byte aligned, pos 4-byte");
+    SQ_REQUIRE(X != Y || ((T == 1 || x_token == y_token) && (H == 1 || x_head == y_head)), SQ_ERR_SHAPE,
+               "sq_rope: in place needs the same strides");
+    return hip_status(sq::launch_rope(X, x_token, x_head, pos, freq, T, H, D, rot, layout, transpose != 0, amplitude, Y,
+                                      y_token, y_head, static_cast<hipStream_t>(stream)),
+                      "rope");
+}
+
+int kv_append(const sq_kv_cache* cache, const uint16_t* K, int64_t k_token, int64_t k_head, const uint16_t* V,
+              int64_t v_token, int64_t v_head, const int32_t* cu, const int32_t* lens, const int32_t* table, int32_t T,
+              int32_t B, int32_t max_pages, const int32_t* pos, const double* freq, int32_t rot, int32_t layout,
+              float amplitude, const uint16_t* Q, int64_t q_token, int64_t q_head, int32_t Hq, uint16_t* Qr,
+              int64_t r_token, int64_t r_head, void* stream) {
+    SQ_TRY(check_cache(cache, "kv_append"));
+    const sq_kv_cache& c = *cache;
+    SQ_TRY(check_batch(cache, cu, lens, table, T, B, max_pages, "kv_append"));
+    if (freq) SQ_TRY(check_rotation(rot, layout, amplitude, c.dim, "kv_append"));
+    SQ_REQUIRE(!Q || (freq && Qr), SQ_ERR_NULL, "kv_append: Q needs freq and Qr");
+    SQ_REQUIRE(!Q || (Hq >= 1 && Hq <= 1024), SQ_ERR_SHAPE, "kv_append: Hq=%d: need 1 .. 1024", Hq);
+    SQ_REQUIRE(((int64_t)T / c.page + 2 * (int64_t)B) * c.heads + (Q ? (int64_t)T * Hq * c.dim / 4096 : 0) < kMaxBlocks,
+               SQ_ERR_SHAPE, "kv_append: T=%d B=%d: too many rows for one call", T, B);
+    if (T == 0 || B == 0) return SQ_OK;
+    SQ_TRY(check_strides(k_token, k_head, T, c.heads, c.dim, false, "kv_append", "K"));
+    SQ_TRY(check_strides(v_token, v_head, T, c.heads, c.dim, false, "kv_append", "V"));
+    SQ_REQUIRE(K && V, SQ_ERR_NULL, "kv_append: K and V are required");
+    SQ_REQUIRE(aligned16(K) && aligned16(V) && aligned16(freq) && aligned16(Q) && aligned16(Qr) && aligned4(pos),
+               SQ_ERR_ALIGN, "kv_append: K, V, Q, Qr and freq must be 16-byte aligned, pos 4-byte");
+    if (Q) {
+        SQ_TRY(check_strides(q_token, q_head, T, Hq, c.dim, false, "kv_append", "Q"));
+        SQ_TRY(check_strides(r_token, r_head, T, Hq, c.dim, true, "kv_append", "Qr"));
+        SQ_REQUIRE(Q != Qr || ((T == 1 || q_token == r_token) && (Hq == 1 || q_head == r_head)), SQ_ERR_SHAPE,
+                   "kv_append: rotating Q in place needs the same strides");
+    }
+    return hip_status(
+        sq::launch_kv_append(c.k, c.v, c.k_scale, c.v_scale, c.pages, c.page, c.heads, c.dim, K, k_token, k_head, V,
+                             v_token, v_head, cu, lens, table, pos, T, B, max_pages, freq, freq ? rot : 0, layout,
+                             amplitude, Q, q_token, q_head, Hq, Qr, r_token, r_head, static_cast<hipStream_t>(stream)),
+        "kv_append");
+}
+
+int kv_read(const sq_kv_cache* cache, const int32_t* list, int32_t n, uint16_t* K, uint16_t* V, void* stream) {
+    SQ_TRY(check_cache(cache, "kv_read"));
+    const sq_kv_cache& c = *cache;
+    SQ_REQUIRE(n >= 0 && (int64_t)n * c.heads < kMaxBlocks, SQ_ERR_SHAPE, "kv_read: n=%d: need n heads < 2^24", n);
+    if (n == 0) return SQ_OK;
+    SQ_REQUIRE(list && K && V, SQ_ERR_NULL, "kv_read: list, K and V are required");
+    SQ_REQUIRE(aligned4(list) && aligned16(K) && aligned16(V), SQ_ERR_ALIGN,
+               "kv_read: K and V must be 16-byte aligned, list 4-byte");
+    return hip_status(sq::launch_kv_read(c.k, c.v, c.k_scale, c.v_scale, c.pages, c.page, c.heads, c.dim, list, n, K, V,
+                                         static_cast<hipStream_t>(stream)),
+                      "kv_read");
+}
+
+size_t sq_attn_kv8_workspace_bytes(int32_t T, int32_t B, int32_t Hq, int32_t heads, int32_t dim, int32_t max_len) {
+    if (T <= 0 || B <= 0 || heads <= 0 || Hq <= 0 || Hq % heads || dim <= 0 || max_len < 0) return 0;
+    return round_up(sq::attn_workspace_bytes(T, B, Hq, heads, dim, max_len));
+}
+
+int attn_kv8(const uint16_t* Q, int64_t q_token, int64_t q_head, const sq_kv_cache* cache, const int32_t* cu,
+             const int32_t* lens, const int32_t* table, int32_t T, int32_t B, int32_t max_pages, int32_t Hq,
+             int32_t causal, int32_t window, float scale, uint16_t* O, float* lse, void* ws, size_t ws_bytes,
+             void* stream) {
+    SQ_TRY(check_cache(cache, "attn_kv8"));
+    const sq_kv_cache& c = *cache;
+    SQ_TRY(check_batch(cache, cu, lens, table, T, B, max_pages, "attn_kv8"));
+    SQ_REQUIRE(Hq >= 1 && Hq <= 1024 && Hq % c.heads == 0, SQ_ERR_SHAPE,
+               "attn_kv8: Hq=%d: need a multiple of heads=%d, at most 1024", Hq, c.heads);
+    SQ_REQUIRE((int64_t)T * Hq / 16 + (int64_t)B * c.heads < kMaxBlocks, SQ_ERR_SHAPE,
+               "attn_kv8: T=%d B=%d: too many rows for one call", T, B);
+    SQ_REQUIRE(window >= 0, SQ_ERR_SHAPE, "attn_kv8: window=%d < 0", window);
+    SQ_REQUIRE(isfinite(scale), SQ_ERR_SHAPE, "attn_kv8: the scale is not finite");
+    if (T == 0 || B == 0) return SQ_OK;
+    SQ_TRY(check_strides(q_token, q_head, T, Hq, c.dim, false, "attn_kv8", "Q"));
+    SQ_REQUIRE(Q && O, SQ_ERR_NULL, "attn_kv8: Q and O are required");
+    SQ_REQUIRE(aligned16(Q) && aligned16(O) && aligned16(lse) && aligned16(ws), SQ_ERR_ALIGN,
+               "attn_kv8: pointers must be 16-byte aligned");
+    const size_t need = sq_attn_kv8_workspace_bytes(T, B, Hq, c.heads, c.dim, max_pages * c.page);
+    SQ_REQUIRE(ws_bytes >= need && (need == 0 || ws), SQ_ERR_WORKSPACE, "attn_kv8: workspace %zu B < %zu B", ws_bytes,
+               need);
+    return hip_status(sq::launch_attn(Q, q_token, q_head, c.k, c.v, c.k_scale, c.v_scale, c.pages, c.page, c.heads,
+                                      c.dim, cu, lens, table, T, B, max_pages, Hq, causal != 0, window, scale, O, lse,
+                                      ws, static_cast<hipStream_t>(stream)),
+                      "attn_kv8");
+}
+
+int sq_quantize_weights_group(const uint16_t* W, int32_t N, int32_t K, int32_t group, uint8_t* Wq, uint16_t* s_w,
+                              void* stream) {
+    SQ_TRY(check_group(N, K, group, "sq_quantize_weights_group"));
+    SQ_REQUIRE((int64_t)N * (K / group) < 4 * kMaxBlocks, SQ_ERR_SHAPE,
+               "sq_quantize_weights_group: N=%d: too many groups for one call", N);
+    if (N == 0) return SQ_OK;
+    SQ_REQUIRE(W && Wq && s_w, SQ_ERR_NULL, "sq_quantize_weights_group: W, Wq and s_w are required");
+    SQ_REQUIRE(aligned16(W) && aligned16(Wq) && aligned16(s_w), SQ_ERR_ALIGN,
+               "sq_quantize_weights_group: pointers must be 16-byte aligned");
+    return hip_status(sq::launch_quantize_group(W, N, K, group, Wq, s_w, static_cast<hipStream_t>(stream)),
+                      "quantize_group");
+}
+
+int w4a16_gemm_frag(const uint16_t* X, const uint8_t* Wf, const uint16_t* s_w, int32_t M, int32_t N, int32_t K,
+                    int32_t group, uint16_t* Y, void* stream) {
+    SQ_TRY(check_group(N, K, group, "w4a16_gemm_frag"));
+    SQ_REQUIRE(M >= 0 && M <= 65535 * 16, SQ_ERR_SHAPE, "w4a16_gemm_frag: M=%d: need 0 .. %d rows", M, 65535 * 16);
+    SQ_REQUIRE(sq::frag_weight_bytes(N, K) < ((size_t)1 << 31), SQ_ERR_SHAPE,
+               "w4a16_gemm_frag: the fragment-ordered weights must be under 2 GiB (N=%d K=%d)", N, K);
+    if (M == 0 || N == 0) return SQ_OK;
+    SQ_REQUIRE(X && Wf && s_w && Y, SQ_ERR_NULL, "w4a16_gemm_frag: X, Wf, s_w and Y are required");
+    SQ_REQUIRE(aligned16(X) && aligned16(Wf) && aligned16(s_w) && aligned16(Y), SQ_ERR_ALIGN,
+               "w4a16_gemm_frag: pointers must be 16-byte aligned");
+    return hip_status(sq::launch_w4a16_frag(X, Wf, s_w, M, N, K, group, Y, static_cast<hipStream_t>(stream)),
+                      "w4a16_gemm_frag");
 }
 
 }  // extern "C"

@@ -1,0 +1,226 @@
+"""Work division of the attention over the cache, on the CPU: the package's planning
+code compiled with g++, every worker and every joining workgroup walked as the kernels
+walk them."""
+import ctypes
+import os
+import random
+import subprocess
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+CSRC = os.path.join(ROOT, "paper_2606_04945_amd", "csrc")
+SHIM = r"""
+#include <map>
+#include <set>
+#include <tuple>
+#include <vector>
+#include "attn_plan.hpp"
+using namespace sq;
+
+// 0 if every step of every tile is read once, every split tile is joined from exactly the places written for
+// it, and every index stays inside its bounds; otherwise a number that says what was wrong.
+extern "C" int walk(int T, int B, int heads, int G, int max_len, int causal, int window, int rows, int at_once,
+                    const int* cu, const int* lens, long long* stats) {
+    AttnShape a{T, B, heads, G, max_len, causal, window, rows, 0};
+    a.workers = attn_workers(a, at_once);
+    if (a.workers < 1 || a.workers > at_once) return 1;
+    std::vector<AttnSeq> s;
+    std::vector<int64_t> before;
+    int64_t total = 0;
+    for (int b = 0; b < B; ++b) {
+        s.push_back(attn_seq(a, cu[b], cu[b + 1], lens[b]));
+        if (s[b].s.t0 < 0 || s[b].s.t0 + s[b].s.n > T || s[b].s.n < 0 || s[b].s.len < 0 || s[b].s.len > max_len) return 2;
+        if (s[b].weight < 0 || (s[b].weight == 0) != (s[b].s.n == 0)) return 3;
+        before.push_back(total);
+        total += s[b].weight * heads;
+    }
+    typedef std::tuple<int, int, int> Tile;
+    std::map<Tile, std::vector<int>> read;                 // how often each step is read
+    std::map<Tile, std::set<int>> written;                 // places of partial results
+    std::map<Tile, int> direct;
+    std::set<int> places;
+    int64_t most = 0, least = INT64_MAX;
+    for (int w = 0; w < a.workers; ++w) {
+        int64_t at = attn_start(total, a.workers, w), end = attn_start(total, a.workers, w + 1), did = 0;
+        if (end < at) return 4;
+        if (at >= end) continue;
+        int b = 0;
+        while (before[b] + s[b].weight * heads <= at) ++b;
+        while (at < end) {
+            if (b >= B) return 5;
+            const AttnSeq& q = s[b];
+            if (q.weight == 0) { ++b; continue; }
+            const int h = (int)((at - before[b]) / q.weight);
+            if (h < 0 || h >= heads) return 6;
+            int r = attn_find_tile(q, at - before[b] - h * q.weight);
+            for (; r < q.tiles && at < end; ++r) {
+                const int64_t weight = q.base + q.slope * r, from = before[b] + h * q.weight + attn_before(q, r);
+                const int64_t x0 = at - from, x1 = std::min(end - from, weight);
+                if (x0 < 0 || x0 >= weight || x1 <= x0) return 7;
+                at = from + x1;
+                const AttnSteps st = attn_steps(a, q.s, r);
+                if (st.count < 0 || st.first < 0 || (int64_t)(st.first + st.count) * kAttnStep >= (int64_t)q.s.len + kAttnStep + (st.count == 0 ? (int64_t)1 << 40 : 0)) return 8;
+                const int k0 = attn_cut(x0, weight, st.count), k1 = attn_cut(x1, weight, st.count);
+                const bool whole = k1 - k0 == st.count && (st.count > 0 || x0 == 0);
+                if (k0 == k1 && !whole) continue;
+                Tile t(b, h, r);
+                read[t].resize(st.count);
+                for (int k = k0; k < k1; ++k) ++read[t][k];
+                did += k1 - k0;
+                if (whole) ++direct[t];
+                else {
+                    const int place = attn_place(w, x0 > 0);
+                    if (place < 0 || place >= 2 * a.workers || !places.insert(place).second) return 9;
+                    written[t].insert(place);
+                }
+            }
+            if (r == q.tiles && at - before[b] >= q.weight * heads) ++b;
+        }
+        most = std::max(most, did);
+        least = std::min(least, did);
+    }
+    int64_t slots = attn_tile_slots(a);
+    long long split = 0;
+    for (int b = 0; b < B; ++b) {
+        const AttnSeq& q = s[b];
+        for (int h = 0; h < heads; ++h)
+            for (int r = 0; r < q.tiles; ++r) {
+                Tile t(b, h, r);
+                const AttnSteps st = attn_steps(a, q.s, r);
+                const auto& c = read[t];
+                if ((int)c.size() != st.count) return 10;
+                for (int x : c) if (x != 1) return 11;
+                // the steps hold every visible key of every row of the tile
+                for (int64_t row = (int64_t)r * rows; row < std::min<int64_t>((int64_t)(r + 1) * rows, (int64_t)q.s.n * G); ++row) {
+                    const int p = q.s.off + (int)(row / G), lo = attn_lo(a, p), hi = attn_hi(a, q.s, p);
+                    if (hi > lo && (lo < st.first * kAttnStep || hi > (st.first + st.count) * kAttnStep)) return 12;
+                }
+                // what the joining workgroup finds
+                const int64_t item = list_start(q.s.t0, b, G, rows, 1) + r;
+                if (item * heads + h >= slots) return 13;
+                int lo = 0, hi = B - 1;
+                while (lo < hi) {
+                    const int mid = (lo + hi + 1) / 2, cm = std::min(std::max(cu[mid], 0), T);
+                    if (list_start(cm, mid, G, rows, 1) <= item) lo = mid; else hi = mid - 1;
+                }
+                if (lo != b) return 14;
+                const int64_t from = before[b] + h * q.weight + attn_before(q, r), weight = q.base + q.slope * r;
+                const int w0 = attn_worker(total, a.workers, from), w1 = attn_worker(total, a.workers, from + weight - 1);
+                std::set<int> join;
+                bool alone = st.count <= 1 || w0 == w1;
+                for (int w = w0; w <= w1 && !alone; ++w) {
+                    const int64_t x0 = attn_start(total, a.workers, w) - from;
+                    const int64_t x1 = std::min(attn_start(total, a.workers, w + 1) - from, weight);
+                    const int k0 = attn_cut(x0, weight, st.count), k1 = attn_cut(x1, weight, st.count);
+                    alone = k1 - k0 == st.count;
+                    if (k1 > k0) join.insert(attn_place(w, x0 > 0));
+                }
+                if (alone ? direct[t] != 1 || !written[t].empty() : direct[t] != 0 || join != written[t]) return 15;
+                split += !alone;
+            }
+    }
+    stats[0] = most; stats[1] = least; stats[2] = split; stats[3] = a.workers;
+    return 0;
+}
+
+extern "C" int touched(int T, int B, int max_len, int page, const int* cu, const int* lens) {
+    std::set<std::pair<int64_t, int>> seen;
+    for (int b = 0; b < B; ++b) {
+        const Seq s = make_seq(cu[b], cu[b + 1], lens[b], T, max_len);
+        const int n = touched_count(s, page);
+        for (int j = 0; j < n; ++j) {
+            const int64_t item = list_start(s.t0, b, 1, page, 2) + j;
+            if (item < 0 || item >= touched_slots(T, B, page)) return 1;
+            int lo = 0, hi = B - 1;
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) / 2, cm = std::min(std::max(cu[mid], 0), T);
+                if (list_start(cm, mid, 1, page, 2) <= item) lo = mid; else hi = mid - 1;
+            }
+            if (lo != b) return 2;
+            const int blk = touched_first(s, page) + j;
+            if (blk * (int64_t)page >= max_len || blk < 0) return 3;
+            if (std::max(s.off, blk * page) >= std::min(s.len, (blk + 1) * page)) return 4;
+        }
+    }
+    return 0;
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def plan(tmp_path_factory):
+    d = tmp_path_factory.mktemp("attn_plan")
+    (d / "shim.cpp").write_text("#include <algorithm>\n" + SHIM)
+    so = str(d / "shim.so")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", "-I", CSRC, str(d / "shim.cpp"), "-o", so],
+                   check=True)
+    return ctypes.CDLL(so)
+
+
+def ints(v):
+    return (ctypes.c_int * len(v))(*v)
+
+
+def walk(plan, T, B, heads, G, max_len, causal, window, rows, at_once, cu, lens):
+    stats = (ctypes.c_longlong * 4)()
+    rc = plan.walk(T, B, heads, G, max_len, causal, window, rows, at_once, ints(cu), ints(lens), stats)
+    return rc, list(stats)
+
+
+def batch(rng, most_new, most_old, B):
+    cu, lens = [0], []
+    for _ in range(B):
+        n = rng.choice([0, 1, 1, rng.randint(0, most_new)])
+        cu.append(cu[-1] + n)
+        lens.append(max(0, rng.choice([n, n + rng.randint(0, most_old), rng.randint(0, most_old)])))
+    return cu, lens
+
+
+@pytest.mark.parametrize("seed", range(300))
+def test_every_step_once(plan, seed):
+    rng = random.Random(seed)
+    B = rng.choice([1, 1, 2, 7, 70])
+    cu, lens = batch(rng, rng.choice([1, 5, 200]), rng.choice([3, 200, 3000]), B)
+    T = cu[-1] + rng.randint(0, 4)
+    max_len = max(lens) + rng.choice([0, 1, 100, 10000])
+    rc, _ = walk(plan, T, B, rng.choice([1, 2, 8]), rng.choice([1, 3, 7, 20]), max_len, rng.randint(0, 1),
+                 rng.choice([0, 0, 1, 50, 700]), rng.choice([16, 64, 128]), rng.choice([1, 8, 512, 2048]), cu, lens)
+    assert rc == 0
+
+
+@pytest.mark.parametrize("seed", range(100))
+def test_any_index_values_stay_inside(plan, seed):
+    """Rows, lengths of any value: nothing outside the bounds (a tile then may be read by nobody or twice)."""
+    rng = random.Random(1000 + seed)
+    B = rng.choice([1, 3, 9])
+    wild = [-2 ** 31, -1, 0, 3, 17, 1000, 2 ** 31 - 1]
+    cu = [rng.choice(wild) for _ in range(B + 1)]
+    lens = [rng.choice(wild) for _ in range(B)]
+    rc, _ = walk(plan, 20, B, 2, 3, 500, seed % 2, rng.choice([0, 9]), 16, 64, cu, lens)
+    assert rc in (0, 10, 11, 13, 14, 15)
+    assert plan.touched(20, B, 500, 16, ints(cu), ints(lens)) in (0, 1, 2)
+
+
+@pytest.mark.parametrize("seed", range(200))
+def test_every_touched_page_has_a_place(plan, seed):
+    rng = random.Random(seed)
+    B = rng.choice([1, 2, 7, 70])
+    cu, lens = batch(rng, rng.choice([1, 5, 300]), rng.choice([3, 200, 3000]), B)
+    assert plan.touched(cu[-1], B, max(lens) + 64, rng.choice([16, 32, 64, 128]), ints(cu), ints(lens)) == 0
+
+
+def test_load_is_even(plan):
+    """One long sequence among short ones: no worker reads more than its share and a step or two."""
+    lens = [100000] + [50] * 31
+    rc, (most, least, split, workers) = walk(plan, 32, 32, 8, 7, 131072, 1, 0, 16, 2048, list(range(33)), lens)
+    steps = 8 * sum(-(-L // 64) for L in lens)
+    assert rc == 0 and workers == 2048 and split == 8
+    assert most <= steps / workers + 3
+
+
+def test_largest_sizes_do_not_overflow(plan):
+    """Weights stay in 64 bits at the limits the interface accepts."""
+    T, heads, G, max_len = 1 << 20, 1, 16, 1 << 28
+    rc, _ = walk(plan, T, 1, heads, G, max_len, 1, 0, 128, 4, [0, 1 << 10], [max_len])
+    assert rc == 0

@@ -1,0 +1,87 @@
+"""Weight-only 4-bit products against the oracle.
+
+Tolerance: one rounding to fp16 of an fp32 sum of K exact products (each addition and
+the group's scale 2^-24 of the sum of magnitudes)."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2606_04945_amd as sq
+from attn_cases import normal
+from gpu_util import assert_bits, dev, host, pack_codes
+from oracle import attn as A
+from oracle import frag as F
+
+pytestmark = pytest.mark.gpu
+
+
+def check(Y, X, codes, s, group):
+    y, mass = A.w4a16(X, codes, s, group)
+    K = X.shape[1]
+    tol = 2.0 ** -11 * np.abs(y) + 2.0 ** -25 + (K + 4) * 2.0 ** -24 * mass
+    g = host(Y).astype(np.float64)
+    assert g.shape == y.shape and (np.abs(g - y) <= tol).all(), (np.abs(g - y) / tol).max()
+
+
+@pytest.mark.parametrize("N,K,group", [(8, 64, 32), (24, 192, 64), (40, 256, 128), (16, 384, 384), (56, 128, 32)])
+def test_quantiser_bit_exact(N, K, group):
+    rng = np.random.default_rng(N + K)
+    W = normal(rng, N, K, scale=0.02)
+    W[0] = 0
+    W[1, :group] = 65504
+    W[2] = 6e-8                                       # scales that are subnormal or zero
+    W[3] *= np.float16(1e-3)
+    Wq, s = sq.quantize_weights_group(dev(W), group)
+    codes, rs = A.quantize_group(W, group)
+    assert_bits(host(s), rs, "scales")
+    assert_bits(host(Wq), pack_codes(codes), "codes")
+
+
+SHAPES = [
+    (1, 8, 64, 32), (1, 4096, 4096, 128), (1, 24, 192, 64), (3, 40, 320, 32), (16, 520, 1024, 128),
+    (17, 264, 1152, 384), (5, 3584, 18944, 64), (33, 72, 2048, 1024), (64, 136, 640, 640), (65, 16, 256, 128),
+    (130, 1032, 576, 32), (2, 12288, 512, 64), (31, 16392, 128, 128),
+]
+
+
+@pytest.mark.parametrize("M,N,K,group", SHAPES)
+def test_product(M, N, K, group):
+    rng = np.random.default_rng(M + N + K)
+    codes = rng.integers(-8, 8, (N, K))
+    s = rng.uniform(1e-3, 2e-2, (K // group, N)).astype(np.float16)
+    X = normal(rng, M, K)
+    Wf = dev(F.to_frag(pack_codes(codes), K))
+    Y = torch.full((M + 1, N), 7.0, dtype=torch.float16, device="cuda")
+    got = sq.w4a16_gemm_frag(dev(X), Wf, dev(s), Y=Y[:M])
+    check(got, X, codes, s, group)
+    assert (host(Y)[M] == 7).all()
+    assert_bits(host(sq.w4a16_gemm_frag(dev(X), Wf, dev(s))), host(got), "again")
+
+
+def test_quantise_then_multiply():
+    rng = np.random.default_rng(1)
+    W, X = normal(rng, 264, 512, scale=0.02), normal(rng, 4, 512)
+    Wq, s = sq.quantize_weights_group(dev(W), 64)
+    Y = sq.w4a16_gemm_frag(dev(X), sq.weights_to_frag(Wq), s)
+    codes, rs = A.quantize_group(W, 64)
+    check(Y, X, codes, rs, 64)
+    full = X.astype(np.float64) @ W.astype(np.float64).T
+    assert np.linalg.norm(host(Y) - full) < 0.15 * np.linalg.norm(full)       # 4 bits: half a step of absmax / 7
+
+
+def test_large_sums_and_padding():
+    """The largest products, an overflow to infinity, and NaN in X stays in its row."""
+    K, N = 192, 24
+    codes = np.full((N, K), -8)
+    s = np.full((K // 64, N), 1.0, np.float16)
+    X = np.full((3, K), 40.0, np.float16)
+    X[1] = 65504
+    X[2, 5] = np.nan
+    Y = host(sq.w4a16_gemm_frag(dev(X), dev(F.to_frag(pack_codes(codes), K)), dev(s)))
+    assert (Y[0] == -8 * 40 * K).all() and np.isneginf(Y[1]).all() and np.isnan(Y[2]).all()
+
+
+def test_empty():
+    s = torch.zeros(2, 16, dtype=torch.float16, device="cuda")
+    Wf = torch.zeros(1, 1, 1024, dtype=torch.uint8, device="cuda")
+    assert sq.w4a16_gemm_frag(torch.zeros(0, 128, dtype=torch.float16, device="cuda"), Wf, s).shape == (0, 16)
