@@ -1,0 +1,273 @@
+// Attention over the paged 8-bit cache: what its kernels share.
+//
+// out = sum_j w_j v_j with w = softmax(scale q . k_j) over the visible keys, one
+// pass over the keys in steps of 64.  Codes go to the fp16 matrix cores as they
+// are, every int8 being an fp16; a page's key scale multiplies its logits in fp32.
+// Its value scale s goes into the weight: with x the logit times log2 e,
+//   w = 2^(x + log2 s - m),  O = sum w code,  l = sum w / s,  out = O / l,
+// and m a running reference close to the largest x + log2 s, so that a weight is
+// rounded to fp16 relative to the row's largest contribution however the scales
+// differ, and the rounding of log2 s cancels between O and l.  Where the reference
+// rises to m', O and l are multiplied by 2^(m - m').
+//
+// Both products are formed transposed, S^T = K Q^T and O^T = V^T P^T: a lane then
+// has one query's logits, which are where the second product wants that query's
+// weights, if the keys of a step are dealt to matrix rows so that both agree.
+// Softmax weights never leave their lane, and keys ([token][D]) and values
+// ([D][token]) are row operands as they are stored.
+#pragma once
+#include "attn_plan.hpp"
+#include "tile_common.hpp"
+
+namespace sq {
+
+struct AttnArgs {
+    AttnShape a;
+    const uint16_t* Q;
+    int64_t q_token, q_head;
+    const int8_t *k, *v;
+    const float *k_scale, *v_scale;
+    int pages, page, shift, D;      // page = 1 << shift
+    const int32_t *cu, *lens, *table;
+    int max_pages;
+    float scale;                    // its magnitude, times log2 e
+    uint32_t flip;                  // sign bits of a pair of halves where the scale is negative
+    uint16_t* O;
+    float* lse;
+    float* ws;
+};
+
+hipError_t launch_attn_wave(const AttnArgs& p, hipStream_t st);
+hipError_t launch_attn_tile(const AttnArgs& p, hipStream_t st);
+
+namespace {
+
+typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+typedef float f2 __attribute__((ext_vector_type(2)));
+typedef float f4 __attribute__((ext_vector_type(4)));
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kNone = -__builtin_inff();
+
+// Sum over the lanes up to this one: shifts within rows of 16 lanes, then the rows'
+// last lanes spread to the rows after them.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int64_t add_shifted(int64_t v) {
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, ROWS, 0xf, true);
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)((uint64_t)v >> 32), CTRL, ROWS, 0xf, true);
+    return v + (int64_t)(((uint64_t)hi << 32) | lo);
+}
+__device__ __forceinline__ int64_t wave_scan(int64_t v) {
+    v = add_shifted<0x111, 0xf>(v);      // row_shr 1, 2, 4, 8
+    v = add_shifted<0x112, 0xf>(v);
+    v = add_shifted<0x114, 0xf>(v);
+    v = add_shifted<0x118, 0xf>(v);
+    v = add_shifted<0x142, 0xa>(v);      // lane 15 of a row to the next row, into rows 1 and 3
+    return add_shifted<0x143, 0xc>(v);   // lane 31 into rows 2 and 3
+}
+__device__ __forceinline__ int64_t lane_value(int64_t v, int lane) {
+    const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)v, lane);
+    const uint32_t hi = __builtin_amdgcn_readlane((int)(uint32_t)((uint64_t)v >> 32), lane);
+    return (int64_t)(((uint64_t)hi << 32) | lo);
+}
+
+// 64 sequences of the batch, one a lane (none past the last: no rows).
+struct Group {
+    int c0, c1, len;
+};
+__device__ __forceinline__ Group load_group(const AttnArgs& p, int b0, int lane) {
+    const int b = b0 + lane, at = min(b, p.a.B - 1);
+    const Group g{p.cu[at], p.cu[at + 1], p.lens[at]};
+    return b < p.a.B ? g : Group{p.a.T, p.a.T, 0};
+}
+__device__ __forceinline__ AttnSeq group_seq(const AttnArgs& p, const Group& g) {
+    return attn_seq(p.a, g.c0, g.c1, g.len);
+}
+__device__ __forceinline__ AttnSeq lane_seq(const AttnArgs& p, const Group& g, int lane) {
+    return attn_seq(p.a, __builtin_amdgcn_readlane(g.c0, lane), __builtin_amdgcn_readlane(g.c1, lane),
+                    __builtin_amdgcn_readlane(g.len, lane));
+}
+
+// Walks the batch 64 sequences at a time: the group that holds the current sequence,
+// loaded once for all of them.
+struct Batch {
+    Group g;
+    int b0;
+    __device__ __forceinline__ AttnSeq seq(const AttnArgs& p, int b, int lane) {
+        if ((b & ~(kWave - 1)) != b0) {
+            b0 = b & ~(kWave - 1);
+            g = load_group(p, b0, lane);
+        }
+        return lane_seq(p, g, b - b0);
+    }
+};
+
+// What every workgroup works out first: the weight of all tiles, and whether the
+// batch is read tile by tile.
+struct Survey {
+    int64_t total;
+    bool direct;
+};
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int64_t max_shifted(int64_t v) {
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, ROWS, 0xf, true);
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)((uint64_t)v >> 32), CTRL, ROWS, 0xf, true);
+    return max(v, (int64_t)(((uint64_t)hi << 32) | lo));
+}
+__device__ __forceinline__ int64_t wave_max64(int64_t v) {   // of values >= 0
+    v = max_shifted<0x111, 0xf>(v);
+    v = max_shifted<0x112, 0xf>(v);
+    v = max_shifted<0x114, 0xf>(v);
+    v = max_shifted<0x118, 0xf>(v);
+    v = max_shifted<0x142, 0xa>(v);
+    return lane_value(max_shifted<0x143, 0xc>(v), kWave - 1);
+}
+__device__ __forceinline__ Survey survey(const AttnArgs& p, const Group& first, int lane) {
+    if (attn_always_direct(p.a)) return {0, true};
+    int64_t total = 0, most = 0;
+    Group g = first;
+    for (int b0 = 0;;) {
+        const AttnSeq q = group_seq(p, g);
+        total += lane_value(wave_scan(q.weight), kWave - 1);
+        const int64_t last = q.tiles > 0 ? q.base + q.slope * (q.tiles - 1) : 0;
+        most = max(most, wave_max64(last));
+        b0 += kWave;
+        if (b0 >= p.a.B) break;
+        g = load_group(p, b0, lane);
+    }
+    total *= p.a.heads;
+    return {total, attn_direct(p.a, total, most)};
+}
+
+// A worker's part of the weight, [at, end), the sequence it begins in and the
+// weight before that sequence.
+struct Share {
+    int64_t at, end, before;
+    int b;
+};
+__device__ __forceinline__ Share find_share(const AttnArgs& p, int64_t total, Batch& batch, int worker, int lane) {
+    const AttnCut cut = attn_cut_work(total, p.a.workers);
+    Share s{attn_start(cut, worker), attn_start(cut, worker + 1), 0, p.a.B};
+    for (int b0 = 0; b0 < p.a.B; b0 += kWave) {
+        if (b0) batch = {load_group(p, b0, lane), b0};
+        const int64_t w = group_seq(p, batch.g).weight, upto = wave_scan(w);
+        const uint64_t past = __ballot(s.before + upto * p.a.heads > s.at);
+        if (past) {
+            const int i = __builtin_ctzll(past);
+            s.b = b0 + i;
+            s.before += lane_value(upto - w, i) * p.a.heads;
+            break;
+        }
+        s.before += lane_value(upto, kWave - 1) * p.a.heads;
+    }
+    return s;
+}
+
+// The sequence whose list of tiles holds place `item`: the last whose list starts
+// at or before it (list starts do not decrease); and the weight of those before it,
+// where asked.
+struct Listed {
+    int b;
+    AttnSeq q;
+    int64_t before;
+};
+template <bool WEIGHTS>
+__device__ __forceinline__ Listed find_listed(const AttnArgs& p, int64_t item, const Group& first, int lane) {
+    Listed r{};
+    int64_t done = 0;
+    Group g = first;
+    for (int b0 = 0;;) {
+        const bool at = b0 + lane < p.a.B && list_start(min(max(g.c0, 0), p.a.T), b0 + lane, p.a.G, p.a.rows, 1) <= item;
+        const int n = __popcll(__ballot(at));
+        if (n > 0) {
+            r.b = b0 + n - 1;
+            r.q = lane_seq(p, g, n - 1);
+        }
+        if (WEIGHTS) {
+            const int64_t w = group_seq(p, g).weight, upto = wave_scan(w);
+            if (n > 0) r.before = (done + lane_value(upto - w, n - 1)) * p.a.heads;
+            done += lane_value(upto, kWave - 1);
+        }
+        b0 += kWave;
+        if (n < kWave || b0 >= p.a.B) return r;
+        g = load_group(p, b0, lane);
+    }
+}
+
+// Worker of a workgroup: dispatch goes round the XCDs, and neighbouring workers read
+// the same keys, so each XCD gets a run of them.
+__device__ __forceinline__ int xcd_worker(int L, int W) {
+    const int x = L % kXcds, base = W / kXcds, rem = W % kXcds;
+    return x * base + (x < rem ? x : rem) + L / kXcds;
+}
+
+// From one tile of a worker's part to the next: the next row tile, or a new place to
+// find (fresh) in the next head or sequence.
+__device__ __forceinline__ void advance(const AttnArgs& p, const AttnSeq& q, Share& s, int& r, bool& fresh) {
+    if (++r < q.tiles) return;
+    fresh = true;
+    if (s.at - s.before >= q.weight * p.a.heads) {
+        s.before += q.weight * p.a.heads;
+        ++s.b;
+    }
+}
+
+// 8 int8 codes as 8 halves, exactly: with the sign bit flipped a code is a byte
+// u = code + 128, the half 0x6400 | u is 1024 + u, and 1152 comes off.
+__device__ __forceinline__ h8 to_halves(uint32_t w0, uint32_t w1) {
+    const h2 bias = {(_Float16)1152.0f, (_Float16)1152.0f};
+    const uint32_t u0 = w0 ^ 0x80808080u, u1 = w1 ^ 0x80808080u;
+    const uint32_t x[4] = {__builtin_amdgcn_perm(0x64646464u, u0, 0x04010400u),
+                           __builtin_amdgcn_perm(0x64646464u, u0, 0x04030402u),
+                           __builtin_amdgcn_perm(0x64646464u, u1, 0x04010400u),
+                           __builtin_amdgcn_perm(0x64646464u, u1, 0x04030402u)};
+    h8 r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const h2 t = __builtin_bit_cast(h2, x[i]) - bias;
+        r[2 * i] = t[0];
+        r[2 * i + 1] = t[1];
+    }
+    return r;
+}
+
+// A hidden key's product and the reference of a row that has seen no key.  A hidden
+// key's logit is below -1e13 for any key scale (those count as 1e-25 at least), far
+// below the reference, so its weight is 0 without a test; no real logit comes near.
+constexpr float kHidden = -3e38f, kUnseen = -1e12f;
+
+// What a block of 16 keys (one page) multiplies: logits by ks, and w by 2^lv with
+// 1 / s = iv.  Keys of no page, or past the length, take no part: lv = -inf.  A value
+// scale below 2^-100, 0 included, counts as that: its contribution to an fp16 result
+// is 0 either way.  The limits also keep infinite and NaN scales of hidden keys from
+// spoiling a weight of 0.
+struct BlockScale {
+    float ks, lv, iv;
+};
+__device__ __forceinline__ BlockScale block_scale(bool in, float ks, float vs, float scale) {
+    const float s = fminf(fmaxf(vs, 0x1p-100f), 3e38f);
+    const float k = fminf(fmaxf(ks * scale, 1e-25f), 3e38f);
+    return {in ? k : 0.0f, in ? __builtin_amdgcn_logf(s) : kNone, in ? 1.0f / s : 0.0f};
+}
+
+// a negative scale's sign goes into the queries, so that larger products are larger logits
+__device__ __forceinline__ h8 load_query(const uint16_t* q, uint32_t flip) {
+    const v4i x = *reinterpret_cast<const v4i*>(q);
+    return __builtin_bit_cast(h8, x ^ (int)flip);
+}
+
+// four results of a row as fp16
+__device__ __forceinline__ void store_result(uint16_t* o, f4 x, float inv) {
+    uint2 w;
+    w.x = (uint32_t)f2h(x[0] * inv) | ((uint32_t)f2h(x[1] * inv) << 16);
+    w.y = (uint32_t)f2h(x[2] * inv) | ((uint32_t)f2h(x[3] * inv) << 16);
+    *reinterpret_cast<uint2*>(o) = w;
+}
+
+__device__ __forceinline__ float result_lse(float m, float l) {
+    return l > 0.0f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : kNone;
+}
+
+}  // namespace
+}  // namespace sq

@@ -20,12 +20,20 @@ namespace sq {
 
 constexpr int kAttnStep = 64;     // keys per step
 
+// a / b for 0 <= a, 0 < b.  Weights of a usual batch fit 32 bits, where a division
+// is several times as fast.
+SQ_HD int64_t divide(int64_t a, int64_t b) {
+    return ((uint64_t)a | (uint64_t)b) >> 32 ? a / b : (int64_t)((uint32_t)a / (uint32_t)b);
+}
+
 struct AttnShape {
     int T, B, heads, G;           // query rows, sequences, key heads, query heads per key head
     int max_len;                  // positions a page table row holds
     int causal, window;
     int rows;                     // rows per tile
-    int workers;
+    int groups;                   // workgroups that run at once
+    int workers;                  // workers that share the work where tiles are split
+    int join;                     // keys whose reading takes as long as the joining kernel
 };
 
 struct AttnSeq {
@@ -37,7 +45,7 @@ struct AttnSeq {
 SQ_HD AttnSeq attn_seq(const AttnShape& a, int c0, int c1, int len) {
     AttnSeq q;
     q.s = make_seq(c0, c1, len, a.T, a.max_len);
-    q.tiles = (int)(((int64_t)q.s.n * a.G + a.rows - 1) / a.rows);
+    q.tiles = (q.s.n * a.G + a.rows - 1) / a.rows;      // T G is below 2^28
     if (a.causal && !a.window) {
         q.slope = a.rows;
         q.base = (int64_t)a.G * ((q.s.off > 0 ? q.s.off : 0) + kAttnStep) + a.rows;
@@ -78,28 +86,49 @@ struct AttnSteps {
     int first, count;
 };
 SQ_HD AttnSteps attn_steps(const AttnShape& a, const Seq& s, int r) {
-    const int64_t row0 = (int64_t)r * a.rows, end = (int64_t)s.n * a.G;
-    const int64_t last = row0 + a.rows < end ? row0 + a.rows - 1 : end - 1;
-    const int lo = attn_lo(a, s.off + (int)(row0 / a.G)), hi = attn_hi(a, s, s.off + (int)(last / a.G));
+    const int row0 = r * a.rows, end = s.n * a.G;
+    const int last = row0 + a.rows < end ? row0 + a.rows - 1 : end - 1;
+    const int lo = attn_lo(a, s.off + row0 / a.G), hi = attn_hi(a, s, s.off + last / a.G);
     if (hi <= lo) return {0, 0};
     return {lo / kAttnStep, (hi + kAttnStep - 1) / kAttnStep - lo / kAttnStep};
 }
 
-// Weight positions of worker w: [attn_start(w), attn_start(w + 1)).
-SQ_HD int64_t attn_start(int64_t total, int workers, int w) {
-    const int64_t q = total / workers, rem = total % workers;
-    return w * q + (w < rem ? w : rem);
+// The weight in equal parts: worker w's are positions [attn_start(w), attn_start(w + 1)).
+struct AttnCut {
+    int64_t each, more;           // the first `more` workers have one position more
+};
+SQ_HD AttnCut attn_cut_work(int64_t total, int workers) {
+    const int64_t each = divide(total, workers);
+    return {each, total - each * workers};
 }
+SQ_HD int64_t attn_start(const AttnCut& c, int w) { return w * c.each + (w < c.more ? w : c.more); }
 // The worker whose part holds position x.
-SQ_HD int attn_worker(int64_t total, int workers, int64_t x) {
-    const int64_t q = total / workers, rem = total % workers;
-    return (int)(x < rem * (q + 1) ? x / (q + 1) : rem + (x - rem * (q + 1)) / q);
+SQ_HD int attn_worker(const AttnCut& c, int64_t x) {
+    const int64_t y = x - c.more * (c.each + 1);
+    return (int)(y < 0 ? divide(x, c.each + 1) : c.more + divide(y, c.each));
 }
 
 // Of `count` steps of a tile of weight `weight`, those before fraction x / weight.
 // 0 at 0 and count at weight, so the parts of a tile cover its steps once.
 SQ_HD int attn_cut(int64_t x, int64_t weight, int count) {
-    return x <= 0 ? 0 : x >= weight ? count : (int)((x * count + weight - 1) / weight);
+    return x <= 0 ? 0 : x >= weight ? count : (int)divide(x * count + weight - 1, weight);
+}
+
+// What a worker that stands at position `at` and ends at `end` does of tile r of key
+// head h: steps [k0, k1), where it stands next, whether these are all of the tile's
+// (a tile without steps is its first worker's, which writes zeros), and whether its
+// part begins inside the tile.
+struct AttnPart {
+    int64_t next;
+    int k0, k1;
+    bool whole, inside;
+};
+SQ_HD AttnPart attn_part(const AttnShape& a, const AttnSeq& q, int64_t before, int h, int r, int64_t at, int64_t end) {
+    const int64_t weight = q.base + q.slope * r, from = before + h * q.weight + attn_before(q, r);
+    const int64_t x0 = at - from, x1 = end - from < weight ? end - from : weight;
+    const AttnSteps s = attn_steps(a, q.s, r);
+    const int k0 = attn_cut(x0, weight, s.count), k1 = attn_cut(x1, weight, s.count);
+    return {from + x1, s.first + k0, s.first + k1, k1 - k0 == s.count && (s.count > 0 || x0 == 0), x0 > 0};
 }
 
 // Partial results: two places for each worker, the tile its part begins inside of
@@ -111,15 +140,42 @@ SQ_HD int64_t attn_place_floats(int rows, int D) { return (int64_t)rows * (D + 2
 // Tiles of all sequences and key heads, at most: what the joining kernel's grid covers.
 inline int64_t attn_tile_slots(const AttnShape& a) { return ((int64_t)a.T * a.G / a.rows + a.B) * a.heads; }
 
-// Workers that a call starts: as many as run at once, fewer where the steps cannot
-// be that many.
-inline int attn_workers(const AttnShape& a, int at_once) {
-    const int64_t steps = ((int64_t)a.max_len + kAttnStep - 1) / kAttnStep;
-    const int64_t tiles = attn_tile_slots(a);
-    const int64_t most = tiles > at_once ? at_once : tiles * (steps > 0 ? steps : 1);
-    return (int)(most < 1 ? 1 : most < at_once ? most : at_once);
+// Whether a batch is read with a workgroup for each tile instead, none split and
+// nothing joined (direct).  `total` is all tiles' weight, `most` the largest tile's.
+// Workgroups take tiles as they come free, so the last ends after about total / groups
+// if no tile is longer than that; splitting saves at most most - total / groups, and
+// costs the joining.  Decided by every workgroup, from the lengths: all of them and
+// the joining kernel come to the same answer.
+SQ_HD bool attn_always_direct(const AttnShape& a) { return a.max_len <= a.join; }   // all that the host can tell
+SQ_HD bool attn_direct(const AttnShape& a, int64_t total, int64_t most) {
+    return attn_always_direct(a) || most <= divide(total, a.groups) + (int64_t)a.G * a.join;
 }
 
-constexpr int kAttnWaves = 256 * 8;      // one-wave workers: two for each SIMD of 256 CUs
+// Which kernel a call takes, by what the host knows: rows and the length that a page
+// table row can hold, not the lengths themselves.
+//   up to 16 rows a sequence and key head, on average: tiles of 16
+//   up to 64: tiles of 32
+//   more: tiles of 128
+// The first two read with single waves (four or eight of a workgroup, one workgroup a
+// CU), the last with workgroups of four waves, two a CU.
+constexpr int kAttnCus = 256;
+
+// Workgroups: a place for every tile, and those that share the work.
+inline int64_t attn_grid(const AttnShape& a) {
+    const int64_t tiles = attn_tile_slots(a);
+    return attn_always_direct(a) || tiles > a.groups ? tiles : a.groups;
+}
+
+inline int attn_waves(int rows, int D) { return rows * (D <= 64 ? 64 : D <= 128 ? 128 : 256) <= 16 * 128 ? 8 : 4; }
+
+inline AttnShape attn_shape(int T, int B, int Hq, int heads, int D, int max_len, bool causal, int window) {
+    const int G = Hq / heads;
+    const int64_t rows = (int64_t)T * G;
+    AttnShape a{T, B, heads, G, max_len, causal, window, 0, kAttnCus, 0, 1024};
+    a.rows = rows <= (int64_t)16 * B ? 16 : rows <= (int64_t)64 * B ? 32 : 128;
+    if (a.rows == 128) a.groups = a.workers = D <= 128 ? 2 * kAttnCus : kAttnCus;
+    else a.workers = a.groups * attn_waves(a.rows, D);
+    return a;
+}
 
 }  // namespace sq

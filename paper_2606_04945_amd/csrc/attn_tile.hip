@@ -1,0 +1,329 @@
+// Attention over the paged 8-bit cache for many rows of a key head: a workgroup turns
+// a step's codes to halves once, in LDS, for all of its rows.
+#include "attn_common.hpp"
+
+namespace sq {
+namespace {
+
+typedef float f16v __attribute__((ext_vector_type(16)));
+
+// LDS of the tile kernel: two buffers of a step's keys [64][DP], two of its values
+// [DP][64], as halves.  16-byte chunks of a row are swapped by the row so that 16
+// lanes reading one chunk of 16 rows take 16 different bank groups.
+template <int DP>
+struct TileLds {
+    static constexpr int kKeys = 64 * DP * 2;          // bytes of a buffer, of values too
+    static __device__ __forceinline__ int key_at(int key, int chunk) {
+        return key * (DP * 2) + ((chunk ^ (DP == 64 ? (key >> 1) & 7 : key & 15)) * 16);
+    }
+    static __device__ __forceinline__ int value_at(int d, int chunk) {
+        return d * 128 + ((chunk ^ ((d >> 1) & 7)) * 16);
+    }
+};
+
+template <int I>
+struct Int {
+    static constexpr int value = I;
+};
+
+// One workgroup of four waves has a tile of 128 rows, 32 a wave, whose queries stay in
+// registers.  The matrix instruction is 32 x 32 x 16: an accumulator of S^T has keys
+// 8 (i / 4) + 4 half + i % 4 of a tile of 32, and values are laid in LDS in that
+// order.  While a step is multiplied the next one's codes become halves in the other
+// buffer and those of the one after are requested: one barrier a step.
+//
+// WIDE: a page holds a step (64 or 128 tokens), so a step has one page and one pair of
+// scales; otherwise each block of 16 keys has its own.
+template <int DP, bool WIDE>
+__global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_tile_kernel(AttnArgs p) {
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+    typedef TileLds<DP> L;
+    constexpr int KS = DP / 16, DT = DP / 32, N = DP / 64;   // k steps, value tiles, 16-byte loads a thread of each
+    constexpr int Z = WIDE ? 1 : 4;                          // scales a step
+    const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    const int c = lane % 32, half = lane / 32;
+    const int G = p.a.G, D = p.D, R = p.a.rows;
+    Batch batch{load_group(p, 0, lane), 0};
+    const Survey all = survey(p, batch.g, lane);
+    Share sh{0, 0, 0, 0};
+    AttnSeq q{};
+    AttnPart part{};
+    int b = 0, h = 0, r = 0, worker = 0;
+    bool fresh = true;
+    if (all.direct) {
+        const int64_t tiles = gridDim.x / p.a.heads;
+        const int64_t at = xcd_worker(blockIdx.x, gridDim.x);
+        const int64_t item = at % tiles;               // a head's tiles run on one XCD
+        h = (int)(at / tiles);
+        if (h >= p.a.heads) return;
+        const Listed l = find_listed<false>(p, item, batch.g, lane);
+        b = l.b;
+        q = l.q;
+        const int64_t r64 = item - list_start(q.s.t0, b, G, R, 1);
+        if (r64 < 0 || r64 >= q.tiles) return;
+        r = (int)r64;
+        const AttnSteps steps = attn_steps(p.a, q.s, r);
+        part = {0, steps.first, steps.first + steps.count, true, false};
+    } else {
+        if ((int)blockIdx.x >= p.a.groups) return;
+        worker = xcd_worker(blockIdx.x, p.a.groups);
+        sh = find_share(p, all.total, batch, worker, lane);
+    }
+    for (;;) {
+        if (!all.direct) {                             // the next tile of this worker's part
+            for (;;) {
+                if (sh.at >= sh.end || sh.b >= p.a.B) return;
+                if (fresh) {
+                    q = batch.seq(p, sh.b, lane);
+                    if (q.weight == 0) {
+                        ++sh.b;
+                        continue;
+                    }
+                    h = (int)divide(sh.at - sh.before, q.weight);
+                    r = attn_find_tile(q, sh.at - sh.before - h * q.weight);
+                    fresh = false;
+                }
+                part = attn_part(p.a, q, sh.before, h, r, sh.at, sh.end);
+                b = sh.b;
+                sh.at = part.next;
+                if (part.k0 < part.k1 || part.whole) break;
+                advance(p, q, sh, r, fresh);
+            }
+        }
+        const int rows = q.s.n * G, row = r * R + wave * 32 + c, at_row = min(row, rows - 1);
+        const int pos = q.s.off + at_row / G, qh = h * G + at_row % G, t = q.s.t0 + at_row / G;
+        const int lo = attn_lo(p.a, pos), hi = attn_hi(p.a, q.s, pos);
+        int lo_most = lo, hi_least = hi;               // of the wave's rows
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            lo_most = max(lo_most, __shfl_xor(lo_most, o, kWave));
+            hi_least = min(hi_least, __shfl_xor(hi_least, o, kWave));
+        }
+        lo_most = __builtin_amdgcn_readfirstlane(lo_most);
+        hi_least = __builtin_amdgcn_readfirstlane(hi_least);
+        h8 Q[KS];
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            const int d = 16 * s + 8 * half;
+            Q[s] = d < D ? load_query(p.Q + t * p.q_token + qh * p.q_head + d, p.flip) : h8{};
+        }
+        f16v O[DT];
+#pragma unroll
+        for (int d = 0; d < DT; ++d) O[d] = f16v{};
+        float m = kUnseen, l = 0.0f;
+        const int32_t* table = p.table + (int64_t)b * p.max_pages;
+        const int s0 = part.k0, s1 = part.k1;
+
+        // this thread's part of a step, N pieces of 16 codes; past a head's channels it reads
+        // others again, which meet zero queries or end in rows that are not stored
+        auto page_of = [&](int key) {
+            const int pid = key < q.s.len ? table[key >> p.shift] : -1;
+            return (uint32_t)pid < (uint32_t)p.pages ? pid : -1;
+        };
+        auto head_of = [&](int pid) { return pid >= 0 ? (int64_t)pid * p.a.heads + h : (int64_t)h; };
+        auto fetch_keys = [&](int kt, v4i (&w)[N]) {
+            const int key0 = kt * kAttnStep;
+            const int8_t* base = WIDE ? p.k + (head_of(page_of(key0)) * p.page + (key0 & (p.page - 1))) * D : nullptr;
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                const int e = tid + 256 * n, key = e / (DP / 16), d = min(e % (DP / 16) * 16, D - 16);
+                if (!WIDE)
+                    base = p.k + (head_of(page_of(key0 + key)) * p.page + ((key0 + key) & (p.page - 1)) - key) * D;
+                w[n] = *reinterpret_cast<const v4i*>(base + (uint32_t)(key * D + d));
+            }
+        };
+        auto fetch_values = [&](int kt, v4i (&w)[N]) {
+            const int key0 = kt * kAttnStep;
+            const int u = tid % 4 * 16, key = WIDE ? key0 : key0 + u;
+            const int8_t* base = p.v + head_of(page_of(key)) * D * p.page + (key & (p.page - 1));
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                const int d = min((tid + 256 * n) / 4, D - 1);
+                w[n] = *reinterpret_cast<const v4i*>(base + (uint32_t)(d * p.page + (WIDE ? u : 0)));
+            }
+        };
+        auto place_keys = [&](uint8_t* at, const v4i (&w)[N]) {
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                const int e = tid + 256 * n, key = e / (DP / 16), chunk = e % (DP / 16) * 2;
+                *reinterpret_cast<h8*>(at + L::key_at(key, chunk)) = to_halves((uint32_t)w[n][0], (uint32_t)w[n][1]);
+                *reinterpret_cast<h8*>(at + L::key_at(key, chunk + 1)) = to_halves((uint32_t)w[n][2], (uint32_t)w[n][3]);
+            }
+        };
+        auto place_values = [&](uint8_t* at, const v4i (&w)[N]) {
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                const int e = tid + 256 * n, d = e / 4, chunk = e % 4 * 2;
+                *reinterpret_cast<h8*>(at + L::value_at(d, chunk)) = to_halves((uint32_t)w[n][0], (uint32_t)w[n][2]);
+                *reinterpret_cast<h8*>(at + L::value_at(d, chunk + 1)) = to_halves((uint32_t)w[n][1], (uint32_t)w[n][3]);
+            }
+        };
+        // scales of a step's blocks: requested with its values, used a step later
+        float sk[Z], sv[Z];
+        bool sin[Z];
+        auto fetch_scales = [&](int kt) {
+#pragma unroll
+            for (int z = 0; z < Z; ++z) {
+                const int pid = page_of(kt * kAttnStep + 16 * z);
+                sin[z] = pid >= 0;
+                sk[z] = p.k_scale[head_of(pid)];
+                sv[z] = p.v_scale[head_of(pid)];
+            }
+        };
+        auto first_product = [&](const uint8_t* at, f16v (&S)[2]) {
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                S[y] = f16v{};
+#pragma unroll
+                for (int s = 0; s < KS; ++s)
+                    S[y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+                        *reinterpret_cast<const h8*>(at + L::key_at(32 * y + c, 2 * s + half)), Q[s], S[y], 0, 0, 0);
+            }
+        };
+        v4i kw[N], vw[N];
+        auto step = [&](auto parity, auto last, int kt) {
+            constexpr int A = decltype(parity)::value;
+            constexpr bool kLast = decltype(last)::value;
+            uint8_t *const keys = lds, *const values = lds + 2 * L::kKeys;
+            BlockScale bs[Z];
+#pragma unroll
+            for (int z = 0; z < Z; ++z) bs[z] = block_scale(sin[z], sk[z], sv[z], p.scale);
+            f16v S[2];
+            first_product(keys + A * L::kKeys, S);
+            if (!kLast) fetch_scales(kt + 1);
+            const int key0 = kt * kAttnStep;
+            if (key0 < lo_most || key0 + kAttnStep > hi_least) {
+                int key = key0 + 4 * half;
+                asm volatile("" : "+v"(key));          // keeps these comparisons out of the steps without an edge
+                const uint32_t from = lo - key, span = hi > lo ? hi - lo : 0;
+#pragma unroll
+                for (int y = 0; y < 2; ++y)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        if ((uint32_t)(32 * y + 8 * (e / 4) + e % 4) - from >= span) S[y][e] = kHidden;
+            }
+            float mx = kUnseen;
+#pragma unroll
+            for (int z = 0; z < 4; z += 4 / Z) {
+                float bm = S[z / 2][8 * (z % 2)];
+#pragma unroll
+                for (int e = 1; e < 32 / Z; ++e) bm = fmaxf(bm, S[z / 2 + e / 16][(8 * (z % 2) + e) % 16]);
+                const BlockScale& k = bs[z * Z / 4];
+                mx = fmaxf(mx, __builtin_fmaf(bm, k.ks, k.lv));
+            }
+            mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
+            // the reference may lag behind by 8: weights to 2^8 keep their precision, and the
+            // accumulators are rescaled a few times a row
+            if (__any(mx > m + 8.0f)) {
+                const float mn = fmaxf(m, mx), fade = __builtin_amdgcn_exp2f(m - mn);
+                m = mn;
+                l *= fade;
+#pragma unroll
+                for (int d = 0; d < DT; ++d) O[d] *= fade;
+            }
+            h8 W[4];
+#pragma unroll
+            for (int z = 0; z < Z; ++z) {
+                float sum = 0.0f;
+                const float off = bs[z].lv - m;
+#pragma unroll
+                for (int e = 0; e < 32 / Z; e += 2) {
+                    const int i = z * (32 / Z) + e;
+                    const f2 w = {__builtin_amdgcn_exp2f(__builtin_fmaf(S[i / 16][i % 16], bs[z].ks, off)),
+                                  __builtin_amdgcn_exp2f(__builtin_fmaf(S[i / 16][i % 16 + 1], bs[z].ks, off))};
+                    sum += w[0];
+                    sum += w[1];
+                    const h2 x = __builtin_convertvector(w, h2);
+                    W[i / 8][i % 8] = x[0];
+                    W[i / 8][i % 8 + 1] = x[1];
+                }
+                l = __builtin_fmaf(sum, bs[z].iv, l);
+            }
+            if (!kLast) {
+                place_keys(keys + (A ^ 1) * L::kKeys, kw);
+                place_values(values + (A ^ 1) * L::kKeys, vw);
+                fetch_keys(min(kt + 2, s1 - 1), kw);
+                fetch_values(min(kt + 2, s1 - 1), vw);
+            }
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+                    O[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+                        *reinterpret_cast<const h8*>(values + A * L::kKeys + L::value_at(32 * d + c, 2 * u + half)), W[u],
+                        O[d], 0, 0, 0);
+            if (!kLast) __syncthreads();
+        };
+        if (s0 < s1) {
+            __syncthreads();                           // the tile before is done with the buffers
+            fetch_scales(s0);
+            fetch_keys(s0, kw);
+            fetch_values(s0, vw);
+            place_keys(lds, kw);
+            fetch_keys(min(s0 + 1, s1 - 1), kw);
+            place_values(lds + 2 * L::kKeys, vw);
+            fetch_values(min(s0 + 1, s1 - 1), vw);
+            __syncthreads();
+            int kt = s0;
+            for (; kt + 2 < s1; kt += 2) {
+                step(Int<0>(), Int<0>(), kt);
+                step(Int<1>(), Int<0>(), kt + 1);
+            }
+            if (kt + 1 < s1) {
+                step(Int<0>(), Int<0>(), kt);
+                step(Int<1>(), Int<1>(), kt + 1);
+            } else {
+                step(Int<0>(), Int<1>(), kt);
+            }
+        }
+        l += __shfl_xor(l, 32, kWave);
+        if (row < rows) {
+            const int64_t o = (int64_t)t * p.a.heads * G + qh;
+            const int lr = wave * 32 + c;
+            const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+            float* ws = part.whole ? nullptr : p.ws + attn_place(worker, part.inside) * attn_place_floats(R, D);
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int ch = 32 * d + 8 * e + 4 * half;
+                    const f4 x{O[d][4 * e], O[d][4 * e + 1], O[d][4 * e + 2], O[d][4 * e + 3]};
+                    if (ch < D) {
+                        if (part.whole) store_result(p.O + o * D + ch, x, inv);
+                        else *reinterpret_cast<f4*>(ws + lr * D + ch) = x;
+                    }
+                }
+            if (half == 0) {
+                if (!part.whole) ws[R * D + lr] = m, ws[R * D + R + lr] = l;
+                else if (p.lse) p.lse[o] = result_lse(m, l);
+            }
+        }
+        if (all.direct) return;
+        advance(p, q, sh, r, fresh);
+    }
+}
+
+template <int DP>
+hipError_t launch(const AttnArgs& p, hipStream_t st) {
+    constexpr int bytes = 4 * TileLds<DP>::kKeys;
+    static std::atomic<int> wide_set[kMaxDevices], set[kMaxDevices];
+    const bool wide = p.page >= kAttnStep;
+    const hipError_t e =
+        wide ? allow_dynamic_lds(reinterpret_cast<const void*>(&attn_tile_kernel<DP, true>), bytes, wide_set)
+             : allow_dynamic_lds(reinterpret_cast<const void*>(&attn_tile_kernel<DP, false>), bytes, set);
+    if (e != hipSuccess) return e;
+    const dim3 grid((unsigned)attn_grid(p.a));
+    if (wide)
+        hipLaunchKernelGGL((attn_tile_kernel<DP, true>), grid, dim3(256), bytes, st, p);
+    else
+        hipLaunchKernelGGL((attn_tile_kernel<DP, false>), grid, dim3(256), bytes, st, p);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_attn_tile(const AttnArgs& p, hipStream_t st) {
+    return p.D <= 64 ? launch<64>(p, st) : p.D <= 128 ? launch<128>(p, st) : launch<256>(p, st);
+}
+
+}  // namespace sq

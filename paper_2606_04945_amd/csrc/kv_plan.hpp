@@ -35,9 +35,10 @@ SQ_HD Seq make_seq(int c0, int c1, int len, int T, int max_len) {
 
 // Where a work list has room for ceil-like counts of every sequence without
 // knowing them: sequence b's part starts at floor(cu[b] per / size) + extra b and
-// has at least ceil(n per / size) + extra - 1 places.  Non-decreasing in b.
+// has at least ceil(n per / size) + extra - 1 places.  Non-decreasing in b.  T per is
+// below 2^31.
 SQ_HD int64_t list_start(int c0, int b, int per, int size, int extra) {
-    return (int64_t)c0 * per / size + (int64_t)extra * b;
+    return c0 * per / size + (int64_t)extra * b;
 }
 
 // Page-sized blocks of the cache that sequence s writes: [first, first + count).

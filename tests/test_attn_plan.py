@@ -22,9 +22,7 @@ using namespace sq;
 // it, and every index stays inside its bounds; otherwise a number that says what was wrong.
 extern "C" int walk(int T, int B, int heads, int G, int max_len, int causal, int window, int rows, int at_once,
                     const int* cu, const int* lens, long long* stats) {
-    AttnShape a{T, B, heads, G, max_len, causal, window, rows, 0};
-    a.workers = attn_workers(a, at_once);
-    if (a.workers < 1 || a.workers > at_once) return 1;
+    const AttnShape a{T, B, heads, G, max_len, causal, window, rows, at_once, at_once, 0};
     std::vector<AttnSeq> s;
     std::vector<int64_t> before;
     int64_t total = 0;
@@ -41,8 +39,10 @@ extern "C" int walk(int T, int B, int heads, int G, int max_len, int causal, int
     std::map<Tile, int> direct;
     std::set<int> places;
     int64_t most = 0, least = INT64_MAX;
+    const AttnCut cut = attn_cut_work(total, a.workers);
+    if (attn_start(cut, 0) != 0 || attn_start(cut, a.workers) != total) return 16;
     for (int w = 0; w < a.workers; ++w) {
-        int64_t at = attn_start(total, a.workers, w), end = attn_start(total, a.workers, w + 1), did = 0;
+        int64_t at = attn_start(cut, w), end = attn_start(cut, w + 1), did = 0;
         if (end < at) return 4;
         if (at >= end) continue;
         int b = 0;
@@ -56,21 +56,21 @@ extern "C" int walk(int T, int B, int heads, int G, int max_len, int causal, int
             int r = attn_find_tile(q, at - before[b] - h * q.weight);
             for (; r < q.tiles && at < end; ++r) {
                 const int64_t weight = q.base + q.slope * r, from = before[b] + h * q.weight + attn_before(q, r);
-                const int64_t x0 = at - from, x1 = std::min(end - from, weight);
-                if (x0 < 0 || x0 >= weight || x1 <= x0) return 7;
-                at = from + x1;
+                if (at < from || at >= from + weight) return 7;
+                const AttnPart part = attn_part(a, q, before[b], h, r, at, end);
+                if (part.next <= at || part.next > end || part.next > from + weight) return 7;
+                at = part.next;
                 const AttnSteps st = attn_steps(a, q.s, r);
-                if (st.count < 0 || st.first < 0 || (int64_t)(st.first + st.count) * kAttnStep >= (int64_t)q.s.len + kAttnStep + (st.count == 0 ? (int64_t)1 << 40 : 0)) return 8;
-                const int k0 = attn_cut(x0, weight, st.count), k1 = attn_cut(x1, weight, st.count);
-                const bool whole = k1 - k0 == st.count && (st.count > 0 || x0 == 0);
-                if (k0 == k1 && !whole) continue;
+                if (st.count < 0 || st.first < 0 || (st.count && (int64_t)(st.first + st.count - 1) * kAttnStep >= q.s.len)) return 8;
+                if (part.k0 == part.k1 && !part.whole) continue;
                 Tile t(b, h, r);
                 read[t].resize(st.count);
-                for (int k = k0; k < k1; ++k) ++read[t][k];
-                did += k1 - k0;
-                if (whole) ++direct[t];
+                if (part.k0 < st.first || part.k1 > st.first + st.count || part.k1 < part.k0) return 17;
+                for (int k = part.k0; k < part.k1; ++k) ++read[t][k - st.first];
+                did += part.k1 - part.k0;
+                if (part.whole) ++direct[t];
                 else {
-                    const int place = attn_place(w, x0 > 0);
+                    const int place = attn_place(w, part.inside);
                     if (place < 0 || place >= 2 * a.workers || !places.insert(place).second) return 9;
                     written[t].insert(place);
                 }
@@ -99,19 +99,15 @@ extern "C" int walk(int T, int B, int heads, int G, int max_len, int causal, int
                 // what the joining workgroup finds
                 const int64_t item = list_start(q.s.t0, b, G, rows, 1) + r;
                 if (item * heads + h >= slots) return 13;
-                int lo = 0, hi = B - 1;
-                while (lo < hi) {
-                    const int mid = (lo + hi + 1) / 2, cm = std::min(std::max(cu[mid], 0), T);
-                    if (list_start(cm, mid, G, rows, 1) <= item) lo = mid; else hi = mid - 1;
-                }
+                int lo = -1;
+                for (int i = 0; i < B; ++i) lo += list_start(std::min(std::max(cu[i], 0), T), i, G, rows, 1) <= item;
                 if (lo != b) return 14;
                 const int64_t from = before[b] + h * q.weight + attn_before(q, r), weight = q.base + q.slope * r;
-                const int w0 = attn_worker(total, a.workers, from), w1 = attn_worker(total, a.workers, from + weight - 1);
+                const int w0 = attn_worker(cut, from), w1 = attn_worker(cut, from + weight - 1);
                 std::set<int> join;
                 bool alone = st.count <= 1 || w0 == w1;
                 for (int w = w0; w <= w1 && !alone; ++w) {
-                    const int64_t x0 = attn_start(total, a.workers, w) - from;
-                    const int64_t x1 = std::min(attn_start(total, a.workers, w + 1) - from, weight);
+                    const int64_t x0 = attn_start(cut, w) - from, x1 = std::min(attn_start(cut, w + 1) - from, weight);
                     const int k0 = attn_cut(x0, weight, st.count), k1 = attn_cut(x1, weight, st.count);
                     alone = k1 - k0 == st.count;
                     if (k1 > k0) join.insert(attn_place(w, x0 > 0));
@@ -122,6 +118,25 @@ extern "C" int walk(int T, int B, int heads, int G, int max_len, int causal, int
     }
     stats[0] = most; stats[1] = least; stats[2] = split; stats[3] = a.workers;
     return 0;
+}
+
+extern "C" int plan(int T, int B, int Hq, int heads, int D, int max_len, int* o) {
+    const AttnShape a = attn_shape(T, B, Hq, heads, D, max_len, true, 0);
+    o[0] = a.groups; o[1] = a.workers; o[2] = attn_always_direct(a);
+    if (attn_grid(a) < attn_tile_slots(a) || (!o[2] && attn_grid(a) < a.groups)) return 0;
+    return a.rows;
+}
+
+// Whether a step of every sequence, `heads` key heads of G query heads, is read without splitting.
+extern "C" int direct(int B, int heads, int G, int max_len, int n, const int* lens) {
+    const AttnShape a = attn_shape(B * n, B, heads * G, heads, 128, max_len, true, 0);
+    int64_t total = 0, most = 0;
+    for (int b = 0; b < B; ++b) {
+        const AttnSeq q = attn_seq(a, b * n, b * n + n, lens[b]);
+        total += q.weight * heads;
+        most = std::max(most, q.base + q.slope * (q.tiles - 1));
+    }
+    return attn_direct(a, total, most);
 }
 
 extern "C" int touched(int T, int B, int max_len, int page, const int* cu, const int* lens) {
@@ -224,3 +239,31 @@ def test_largest_sizes_do_not_overflow(plan):
     T, heads, G, max_len = 1 << 20, 1, 16, 1 << 28
     rc, _ = walk(plan, T, 1, heads, G, max_len, 1, 0, 128, 4, [0, 1 << 10], [max_len])
     assert rc == 0
+
+
+def test_which_kernel(plan):
+    """Rows a tile, workgroups, workers and whether nothing can be split, by rows, heads and room of the page table."""
+    def shape(*a):
+        o = (ctypes.c_int * 3)()
+        return plan.plan(*a, o), *o
+    assert shape(1, 1, 32, 32, 128, 512) == (16, 256, 2048, 1)
+    assert shape(32, 32, 28, 4, 128, 8192) == (16, 256, 2048, 0)
+    assert shape(2, 2, 64, 8, 256, 131072) == (16, 256, 1024, 0)
+    assert shape(8 * 32, 8, 32, 32, 128, 2112) == (32, 256, 1024, 0)
+    assert shape(8 * 32, 8, 32, 32, 64, 320) == (32, 256, 2048, 1)
+    assert shape(8 * 2048, 8, 28, 4, 128, 2048) == (128, 512, 512, 0)
+    assert shape(32, 1, 28, 4, 256, 64) == (128, 256, 256, 1)
+
+
+def test_direct_or_shared(plan):
+    """Tile by tile where no tile is much longer than a workgroup's share, or the difference is small."""
+    def direct(lens, heads, G, n=1, room=1 << 20):
+        return plan.direct(len(lens), heads, G, room, n, ints(lens))
+    assert direct([517], 32, 1)                               # short
+    assert not direct([131072] * 2, 8, 8)                     # 16 tiles of 256 workgroups'
+    assert direct([2000] * 8, 32, 1, 32)                      # a tile a workgroup, even
+    assert not direct([100000] + [100] * 63, 8, 4)            # one long sequence
+    assert direct([3000] * 256, 4, 7) and direct([1500] * 8, 4, 7, 1500)
+    for seed in range(50):                                    # a narrow table: whatever the lengths
+        rng = random.Random(seed)
+        assert direct([rng.randint(0, 1024) for _ in range(rng.randint(1, 9))], 2, 4, rng.choice([1, 40]), 1024)
