@@ -89,19 +89,10 @@ __device__ __forceinline__ AttnSeq lane_seq(const AttnArgs& p, const Group& g, i
                     __builtin_amdgcn_readlane(g.len, lane));
 }
 
-// Walks the batch 64 sequences at a time: the group that holds the current sequence,
-// loaded once for all of them.
-struct Batch {
-    Group g;
-    int b0;
-    __device__ __forceinline__ AttnSeq seq(const AttnArgs& p, int b, int lane) {
-        if ((b & ~(kWave - 1)) != b0) {
-            b0 = b & ~(kWave - 1);
-            g = load_group(p, b0, lane);
-        }
-        return lane_seq(p, g, b - b0);
-    }
-};
+// sequence b, the same for all lanes
+__device__ __forceinline__ AttnSeq scalar_seq(const AttnArgs& p, int b) {
+    return attn_seq(p.a, p.cu[b], p.cu[b + 1], p.lens[b]);
+}
 
 // What every workgroup works out first: the weight of all tiles, and whether the
 // batch is read tile by tile.
@@ -146,12 +137,12 @@ struct Share {
     int64_t at, end, before;
     int b;
 };
-__device__ __forceinline__ Share find_share(const AttnArgs& p, int64_t total, Batch& batch, int worker, int lane) {
+__device__ __forceinline__ Share find_share(const AttnArgs& p, int64_t total, const Group& first, int worker,
+                                            int lane) {
     const AttnCut cut = attn_cut_work(total, p.a.workers);
     Share s{attn_start(cut, worker), attn_start(cut, worker + 1), 0, p.a.B};
     for (int b0 = 0; b0 < p.a.B; b0 += kWave) {
-        if (b0) batch = {load_group(p, b0, lane), b0};
-        const int64_t w = group_seq(p, batch.g).weight, upto = wave_scan(w);
+        const int64_t w = group_seq(p, b0 ? load_group(p, b0, lane) : first).weight, upto = wave_scan(w);
         const uint64_t past = __ballot(s.before + upto * p.a.heads > s.at);
         if (past) {
             const int i = __builtin_ctzll(past);
@@ -202,15 +193,29 @@ __device__ __forceinline__ int xcd_worker(int L, int W) {
     return x * base + (x < rem ? x : rem) + L / kXcds;
 }
 
-// From one tile of a worker's part to the next: the next row tile, or a new place to
-// find (fresh) in the next head or sequence.
-__device__ __forceinline__ void advance(const AttnArgs& p, const AttnSeq& q, Share& s, int& r, bool& fresh) {
-    if (++r < q.tiles) return;
-    fresh = true;
-    if (s.at - s.before >= q.weight * p.a.heads) {
-        s.before += q.weight * p.a.heads;
-        ++s.b;
+// The tile at a worker's position and what it does of it; moves the position on.  False
+// at the end of the worker's part.
+struct Tile {
+    Seq s;
+    int b, h, r;
+    AttnPart part;
+};
+__device__ __forceinline__ bool next_tile(const AttnArgs& p, Share& sh, Tile& t) {
+    while (sh.at < sh.end && sh.b < p.a.B) {
+        const AttnSeq q = scalar_seq(p, sh.b);
+        const int64_t weight = q.weight * p.a.heads;
+        if (sh.at - sh.before >= weight) {             // also a sequence without rows
+            sh.before += weight;
+            ++sh.b;
+            continue;
+        }
+        const int h = (int)divide(sh.at - sh.before, q.weight);
+        const int r = attn_find_tile(q, sh.at - sh.before - h * q.weight);
+        t = {q.s, sh.b, h, r, attn_part(p.a, q, sh.before, h, r, sh.at, sh.end)};
+        sh.at = t.part.next;
+        if (t.part.k0 < t.part.k1 || t.part.whole) return true;
     }
+    return false;
 }
 
 // 8 int8 codes as 8 halves, exactly: with the sign bit flipped a code is a byte

@@ -21,6 +21,13 @@ struct TileLds {
     }
 };
 
+// An offset whose uses are recomputed where they are: the other chunks of a row are an
+// exclusive or away, which costs less than a register each.
+__device__ __forceinline__ int here(int x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
 template <int I>
 struct Int {
     static constexpr int value = I;
@@ -43,56 +50,34 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_tile_kernel(AttnA
     const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int c = lane % 32, half = lane / 32;
     const int G = p.a.G, D = p.D, R = p.a.rows;
-    Batch batch{load_group(p, 0, lane), 0};
-    const Survey all = survey(p, batch.g, lane);
+    const Group first = load_group(p, 0, lane);
+    const Survey all = survey(p, first, lane);
     Share sh{0, 0, 0, 0};
-    AttnSeq q{};
-    AttnPart part{};
-    int b = 0, h = 0, r = 0, worker = 0;
-    bool fresh = true;
+    Tile tile{};
+    int worker = 0;
     if (all.direct) {
         const int64_t tiles = gridDim.x / p.a.heads;
         const int64_t at = xcd_worker(blockIdx.x, gridDim.x);
         const int64_t item = at % tiles;               // a head's tiles run on one XCD
-        h = (int)(at / tiles);
-        if (h >= p.a.heads) return;
-        const Listed l = find_listed<false>(p, item, batch.g, lane);
-        b = l.b;
-        q = l.q;
-        const int64_t r64 = item - list_start(q.s.t0, b, G, R, 1);
-        if (r64 < 0 || r64 >= q.tiles) return;
-        r = (int)r64;
-        const AttnSteps steps = attn_steps(p.a, q.s, r);
-        part = {0, steps.first, steps.first + steps.count, true, false};
+        if (at / tiles >= p.a.heads) return;
+        const Listed l = find_listed<false>(p, item, first, lane);
+        const int64_t r64 = item - list_start(l.q.s.t0, l.b, G, R, 1);
+        if (r64 < 0 || r64 >= l.q.tiles) return;
+        const AttnSteps steps = attn_steps(p.a, l.q.s, (int)r64);
+        tile = {l.q.s, l.b, (int)(at / tiles), (int)r64, {0, steps.first, steps.first + steps.count, true, false}};
     } else {
         if ((int)blockIdx.x >= p.a.groups) return;
         worker = xcd_worker(blockIdx.x, p.a.groups);
-        sh = find_share(p, all.total, batch, worker, lane);
+        sh = find_share(p, all.total, first, worker, lane);
     }
     for (;;) {
-        if (!all.direct) {                             // the next tile of this worker's part
-            for (;;) {
-                if (sh.at >= sh.end || sh.b >= p.a.B) return;
-                if (fresh) {
-                    q = batch.seq(p, sh.b, lane);
-                    if (q.weight == 0) {
-                        ++sh.b;
-                        continue;
-                    }
-                    h = (int)divide(sh.at - sh.before, q.weight);
-                    r = attn_find_tile(q, sh.at - sh.before - h * q.weight);
-                    fresh = false;
-                }
-                part = attn_part(p.a, q, sh.before, h, r, sh.at, sh.end);
-                b = sh.b;
-                sh.at = part.next;
-                if (part.k0 < part.k1 || part.whole) break;
-                advance(p, q, sh, r, fresh);
-            }
-        }
-        const int rows = q.s.n * G, row = r * R + wave * 32 + c, at_row = min(row, rows - 1);
-        const int pos = q.s.off + at_row / G, qh = h * G + at_row % G, t = q.s.t0 + at_row / G;
-        const int lo = attn_lo(p.a, pos), hi = attn_hi(p.a, q.s, pos);
+        if (!all.direct && !next_tile(p, sh, tile)) return;
+        const AttnPart& part = tile.part;
+        const Seq& seq = tile.s;
+        const int h = tile.h;
+        const int rows = seq.n * G, row = tile.r * R + wave * 32 + c, at_row = min(row, rows - 1);
+        const int pos = seq.off + at_row / G, qh = h * G + at_row % G, t = seq.t0 + at_row / G;
+        const int lo = attn_lo(p.a, pos), hi = attn_hi(p.a, seq, pos);
         int lo_most = lo, hi_least = hi;               // of the wave's rows
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) {
@@ -111,13 +96,13 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_tile_kernel(AttnA
 #pragma unroll
         for (int d = 0; d < DT; ++d) O[d] = f16v{};
         float m = kUnseen, l = 0.0f;
-        const int32_t* table = p.table + (int64_t)b * p.max_pages;
+        const int32_t* table = p.table + (int64_t)tile.b * p.max_pages;
         const int s0 = part.k0, s1 = part.k1;
 
         // this thread's part of a step, N pieces of 16 codes; past a head's channels it reads
         // others again, which meet zero queries or end in rows that are not stored
         auto page_of = [&](int key) {
-            const int pid = key < q.s.len ? table[key >> p.shift] : -1;
+            const int pid = key < seq.len ? table[key >> p.shift] : -1;
             return (uint32_t)pid < (uint32_t)p.pages ? pid : -1;
         };
         auto head_of = [&](int pid) { return pid >= 0 ? (int64_t)pid * p.a.heads + h : (int64_t)h; };
@@ -143,19 +128,22 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_tile_kernel(AttnA
             }
         };
         auto place_keys = [&](uint8_t* at, const v4i (&w)[N]) {
+            const int k0 = here(L::key_at(tid / (DP / 16), tid % (DP / 16) * 2));
 #pragma unroll
             for (int n = 0; n < N; ++n) {
-                const int e = tid + 256 * n, key = e / (DP / 16), chunk = e % (DP / 16) * 2;
-                *reinterpret_cast<h8*>(at + L::key_at(key, chunk)) = to_halves((uint32_t)w[n][0], (uint32_t)w[n][1]);
-                *reinterpret_cast<h8*>(at + L::key_at(key, chunk + 1)) = to_halves((uint32_t)w[n][2], (uint32_t)w[n][3]);
+                // 256 pieces on: a multiple of 16 rows, which share their exchange of chunks
+                const int k = k0 + 256 * 16 / DP * n * (DP * 2);
+                *reinterpret_cast<h8*>(at + k) = to_halves((uint32_t)w[n][0], (uint32_t)w[n][1]);
+                *reinterpret_cast<h8*>(at + (k ^ 16)) = to_halves((uint32_t)w[n][2], (uint32_t)w[n][3]);
             }
         };
         auto place_values = [&](uint8_t* at, const v4i (&w)[N]) {
+            const int v0 = here(L::value_at(tid / 4, tid % 4 * 2));
 #pragma unroll
             for (int n = 0; n < N; ++n) {
-                const int e = tid + 256 * n, d = e / 4, chunk = e % 4 * 2;
-                *reinterpret_cast<h8*>(at + L::value_at(d, chunk)) = to_halves((uint32_t)w[n][0], (uint32_t)w[n][2]);
-                *reinterpret_cast<h8*>(at + L::value_at(d, chunk + 1)) = to_halves((uint32_t)w[n][1], (uint32_t)w[n][3]);
+                const int v = v0 + 64 * n * 128;       // 64 channels on
+                *reinterpret_cast<h8*>(at + v) = to_halves((uint32_t)w[n][0], (uint32_t)w[n][2]);
+                *reinterpret_cast<h8*>(at + (v ^ 16)) = to_halves((uint32_t)w[n][1], (uint32_t)w[n][3]);
             }
         };
         // scales of a step's blocks: requested with its values, used a step later
@@ -171,13 +159,14 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_tile_kernel(AttnA
             }
         };
         auto first_product = [&](const uint8_t* at, f16v (&S)[2]) {
+            const int k0 = here(L::key_at(c, half));
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
                 S[y] = f16v{};
 #pragma unroll
                 for (int s = 0; s < KS; ++s)
                     S[y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
-                        *reinterpret_cast<const h8*>(at + L::key_at(32 * y + c, 2 * s + half)), Q[s], S[y], 0, 0, 0);
+                        *reinterpret_cast<const h8*>(at + 32 * y * (DP * 2) + (k0 ^ (32 * s))), Q[s], S[y], 0, 0, 0);
             }
         };
         v4i kw[N], vw[N];
@@ -245,13 +234,14 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_tile_kernel(AttnA
                 fetch_keys(min(kt + 2, s1 - 1), kw);
                 fetch_values(min(kt + 2, s1 - 1), vw);
             }
+            const int v0 = here(L::value_at(c, half));
 #pragma unroll
-            for (int d = 0; d < DT; ++d)
+            for (int u = 0; u < 4; ++u)
 #pragma unroll
-                for (int u = 0; u < 4; ++u)
+                for (int d = 0; d < DT; ++d)
                     O[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
-                        *reinterpret_cast<const h8*>(values + A * L::kKeys + L::value_at(32 * d + c, 2 * u + half)), W[u],
-                        O[d], 0, 0, 0);
+                        *reinterpret_cast<const h8*>(values + A * L::kKeys + 32 * d * 128 + (v0 ^ (32 * u))), W[u], O[d],
+                        0, 0, 0);
             if (!kLast) __syncthreads();
         };
         if (s0 < s1) {
@@ -299,7 +289,6 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_tile_kernel(AttnA
             }
         }
         if (all.direct) return;
-        advance(p, q, sh, r, fresh);
     }
 }
 

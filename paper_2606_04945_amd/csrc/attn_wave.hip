@@ -215,61 +215,36 @@ __global__ __launch_bounds__(NW* kWave) void attn_wave_kernel(AttnArgs p) {
     float* ml = lds + NW * R * LD;                     // [wave][row] m, then l
     const int lane = threadIdx.x % kWave, c = lane % 16, g = lane / 16;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    Batch batch{load_group(p, 0, lane), 0};
-    const Survey all = survey(p, batch.g, lane);
+    const Group first = load_group(p, 0, lane);
+    const Survey all = survey(p, first, lane);
     Share sh{0, 0, 0, 0};
-    AttnSeq q{};
-    AttnPart part{};
-    int b = 0, h = 0, r = 0, worker = 0, stride = 1, count = 0;
-    bool fresh = true;
+    Tile t{};
+    int worker = 0, stride = 1, count = 0;
     if (all.direct) {
         const int64_t item = blockIdx.x / p.a.heads;
-        h = blockIdx.x % p.a.heads;
-        const Listed at = find_listed<false>(p, item, batch.g, lane);
-        b = at.b;
-        q = at.q;
-        const int64_t r64 = item - list_start(q.s.t0, b, p.a.G, R, 1);
-        if (r64 < 0 || r64 >= q.tiles) return;
-        r = (int)r64;
-        const AttnSteps steps = attn_steps(p.a, q.s, r);
+        const Listed at = find_listed<false>(p, item, first, lane);
+        const int64_t r64 = item - list_start(at.q.s.t0, at.b, p.a.G, R, 1);
+        if (r64 < 0 || r64 >= at.q.tiles) return;
+        const AttnSteps steps = attn_steps(p.a, at.q.s, (int)r64);
         count = steps.count;
         stride = NW;
-        part = {0, steps.first + wave, steps.first + steps.count, false, false};
+        t = {at.q.s, at.b, (int)(blockIdx.x % p.a.heads), (int)r64,
+             {0, steps.first + wave, steps.first + steps.count, false, false}};
     } else {
         if ((int)blockIdx.x >= p.a.groups) return;
         worker = xcd_worker(blockIdx.x, p.a.groups) * NW + wave;
-        sh = find_share(p, all.total, batch, worker, lane);
+        sh = find_share(p, all.total, first, worker, lane);
     }
     for (;;) {
-        if (!all.direct) {                             // the next tile of this worker's part
-            for (;;) {
-                if (sh.at >= sh.end || sh.b >= p.a.B) return;
-                if (fresh) {
-                    q = batch.seq(p, sh.b, lane);
-                    if (q.weight == 0) {
-                        ++sh.b;
-                        continue;
-                    }
-                    h = (int)divide(sh.at - sh.before, q.weight);
-                    r = attn_find_tile(q, sh.at - sh.before - h * q.weight);
-                    fresh = false;
-                }
-                part = attn_part(p.a, q, sh.before, h, r, sh.at, sh.end);
-                b = sh.b;
-                sh.at = part.next;
-                if (part.k0 < part.k1 || part.whole) break;
-                advance(p, q, sh, r, fresh);
-            }
-        }
+        if (!all.direct && !next_tile(p, sh, t)) return;
         WaveRows<DP, QT> w;
-        w.begin(p, q.s, h, r, c, g);
-        w.pass(p, q.s, b, h, part.k0, part.k1, stride, c, g);
+        w.begin(p, t.s, t.h, t.r, c, g);
+        w.pass(p, t.s, t.b, t.h, t.part.k0, t.part.k1, stride, c, g);
         if (!all.direct) {
-            if (part.whole)
+            if (t.part.whole)
                 w.store(p, g);
             else
-                w.store_partial(p, p.ws + attn_place(worker, part.inside) * attn_place_floats(R, p.D), c, g);
-            advance(p, q, sh, r, fresh);
+                w.store_partial(p, p.ws + attn_place(worker, t.part.inside) * attn_place_floats(R, p.D), c, g);
             continue;
         }
         const int waves = min(count, NW);              // those that had a step
@@ -288,7 +263,7 @@ __global__ __launch_bounds__(NW* kWave) void attn_wave_kernel(AttnArgs p) {
             }
         }
         __syncthreads();
-        const int rows = min(R, q.s.n * p.a.G - r * R), vecs = p.D / 4;
+        const int rows = min(R, t.s.n * p.a.G - t.r * R), vecs = p.D / 4;
         for (int e = threadIdx.x; e < rows * vecs; e += NW * kWave) {
             const int row = e / vecs, d = e % vecs * 4;
             float m = kUnseen;
@@ -300,8 +275,8 @@ __global__ __launch_bounds__(NW* kWave) void attn_wave_kernel(AttnArgs p) {
                 l = __builtin_fmaf(ml[(NW + v) * R + row], f, l);
                 O += *reinterpret_cast<const f4*>(lds + (v * R + row) * LD + d) * f;
             }
-            const int at = r * R + row;
-            const int64_t o = (int64_t)(q.s.t0 + at / p.a.G) * p.a.heads * p.a.G + h * p.a.G + at % p.a.G;
+            const int at = t.r * R + row;
+            const int64_t o = (int64_t)(t.s.t0 + at / p.a.G) * p.a.heads * p.a.G + t.h * p.a.G + at % p.a.G;
             store_result(p.O + o * p.D + d, O, l > 0.0f ? 1.0f / l : 0.0f);
             if (p.lse && d == 0) p.lse[o] = result_lse(m, l);
         }
