@@ -28,6 +28,10 @@ __device__ __forceinline__ int here(int x) {
     return x;
 }
 
+__device__ __forceinline__ float lane_float(float x, int lane) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), lane));
+}
+
 template <int I>
 struct Int {
     static constexpr int value = I;
@@ -72,9 +76,10 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_tile_kernel(AttnA
     }
     for (;;) {
         if (!all.direct && !next_tile(p, sh, tile)) return;
+        const Seq seq{__builtin_amdgcn_readfirstlane(tile.s.t0), __builtin_amdgcn_readfirstlane(tile.s.n),
+                      __builtin_amdgcn_readfirstlane(tile.s.len), __builtin_amdgcn_readfirstlane(tile.s.off)};
         const AttnPart& part = tile.part;
-        const Seq& seq = tile.s;
-        const int h = tile.h;
+        const int h = __builtin_amdgcn_readfirstlane(tile.h);
         const int rows = seq.n * G, row = tile.r * R + wave * 32 + c, at_row = min(row, rows - 1);
         const int pos = seq.off + at_row / G, qh = h * G + at_row % G, t = seq.t0 + at_row / G;
         const int lo = attn_lo(p.a, pos), hi = attn_hi(p.a, seq, pos);
@@ -96,35 +101,68 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_tile_kernel(AttnA
 #pragma unroll
         for (int d = 0; d < DT; ++d) O[d] = f16v{};
         float m = kUnseen, l = 0.0f;
-        const int32_t* table = p.table + (int64_t)tile.b * p.max_pages;
-        const int s0 = part.k0, s1 = part.k1;
+        const int s0 = __builtin_amdgcn_readfirstlane(part.k0), s1 = __builtin_amdgcn_readfirstlane(part.k1);
 
-        // this thread's part of a step, N pieces of 16 codes; past a head's channels it reads
-        // others again, which meet zero queries or end in rows that are not stored
-        auto page_of = [&](int key) {
-            const int pid = key < seq.len ? table[key >> p.shift] : -1;
-            return (uint32_t)pid < (uint32_t)p.pages ? pid : -1;
-        };
-        auto head_of = [&](int pid) { return pid >= 0 ? (int64_t)pid * p.a.heads + h : (int64_t)h; };
-        auto fetch_keys = [&](int kt, v4i (&w)[N]) {
-            const int key0 = kt * kAttnStep;
-            const int8_t* base = WIDE ? p.k + (head_of(page_of(key0)) * p.page + (key0 & (p.page - 1))) * D : nullptr;
-#pragma unroll
-            for (int n = 0; n < N; ++n) {
-                const int e = tid + 256 * n, key = e / (DP / 16), d = min(e % (DP / 16) * 16, D - 16);
-                if (!WIDE)
-                    base = p.k + (head_of(page_of(key0 + key)) * p.page + ((key0 + key) & (p.page - 1)) - key) * D;
-                w[n] = *reinterpret_cast<const v4i*>(base + (uint32_t)(key * D + d));
+        // 64 page table entries, one a lane, from entry `first_id` on, so that a step finds its
+        // pages without a load of its own to wait for
+        const int32_t* table = p.table + (int64_t)tile.b * p.max_pages;
+        const int held = (seq.len + p.page - 1) >> p.shift;
+        int ids = -1, first_id = -kWave;
+        auto hold_pages = [&](int kt) {
+            const int at = kt * kAttnStep >> p.shift;
+            if (at + (WIDE ? 1 : kAttnStep >> p.shift) - first_id > kWave) {
+                first_id = at;
+                const int id = at + lane < held ? table[at + lane] : -1;
+                ids = (uint32_t)id < (uint32_t)p.pages ? id : -1;
             }
         };
-        auto fetch_values = [&](int kt, v4i (&w)[N]) {
-            const int key0 = kt * kAttnStep;
-            const int u = tid % 4 * 16, key = WIDE ? key0 : key0 + u;
-            const int8_t* base = p.v + head_of(page_of(key)) * D * p.page + (key & (p.page - 1));
+        auto head_of = [&](int pid) { return pid >= 0 ? (int64_t)pid * p.a.heads + h : (int64_t)h; };
+
+        // this thread's part of a step, N pieces of 16 codes; past a head's channels it reads
+        // others again, which meet zero queries or end in rows that are not stored; and the
+        // scales of block lane % 4
+        v4i kw[N], vw[N];
+        float sk[2], sv[2];
+        bool sin[2];
+        auto fetch = [&](int kt, auto parity) {
+            constexpr int A = decltype(parity)::value;
+            hold_pages(kt);
+            const int key0 = kt * kAttnStep, at = (key0 >> p.shift) - first_id;
+            if constexpr (WIDE) {
+                const int pid = __builtin_amdgcn_readlane(ids, at), slot = key0 & (p.page - 1);
+                const int64_t ph = head_of(pid);
+                const int8_t* kb = p.k + (ph * p.page + slot) * D;
+                const int8_t* vb = p.v + ph * p.page * D + slot;
 #pragma unroll
-            for (int n = 0; n < N; ++n) {
-                const int d = min((tid + 256 * n) / 4, D - 1);
-                w[n] = *reinterpret_cast<const v4i*>(base + (uint32_t)(d * p.page + (WIDE ? u : 0)));
+                for (int n = 0; n < N; ++n) {
+                    const int e = tid + 256 * n;
+                    kw[n] = *reinterpret_cast<const v4i*>(
+                        kb + (uint32_t)(e / (DP / 16) * D + min(e % (DP / 16) * 16, D - 16)));
+                }
+#pragma unroll
+                for (int n = 0; n < N; ++n)
+                    vw[n] = *reinterpret_cast<const v4i*>(
+                        vb + (uint32_t)(min(tid / 4 + 64 * n, D - 1) * p.page + tid % 4 * 16));
+                sin[A] = pid >= 0;
+                sk[A] = p.k_scale[ph];
+                sv[A] = p.v_scale[ph];
+            } else {
+                auto lane_page = [&](int key) { return __shfl(ids, at + (key >> p.shift), kWave); };
+#pragma unroll
+                for (int n = 0; n < N; ++n) {
+                    const int e = tid + 256 * n, key = e / (DP / 16), d = min(e % (DP / 16) * 16, D - 16);
+                    kw[n] = *reinterpret_cast<const v4i*>(
+                        p.k + (head_of(lane_page(key)) * p.page + (key & (p.page - 1))) * D + d);
+                }
+                const int u = tid % 4 * 16;
+                const int8_t* vb = p.v + head_of(lane_page(u)) * D * p.page + (u & (p.page - 1));
+#pragma unroll
+                for (int n = 0; n < N; ++n)
+                    vw[n] = *reinterpret_cast<const v4i*>(vb + (uint32_t)(min(tid / 4 + 64 * n, D - 1) * p.page));
+                const int pid = lane_page(lane % 4 * 16);
+                sin[A] = pid >= 0;
+                sk[A] = p.k_scale[head_of(pid)];
+                sv[A] = p.v_scale[head_of(pid)];
             }
         };
         auto place_keys = [&](uint8_t* at, const v4i (&w)[N]) {
@@ -146,18 +184,6 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_tile_kernel(AttnA
                 *reinterpret_cast<h8*>(at + (v ^ 16)) = to_halves((uint32_t)w[n][1], (uint32_t)w[n][3]);
             }
         };
-        // scales of a step's blocks: requested with its values, used a step later
-        float sk[Z], sv[Z];
-        bool sin[Z];
-        auto fetch_scales = [&](int kt) {
-#pragma unroll
-            for (int z = 0; z < Z; ++z) {
-                const int pid = page_of(kt * kAttnStep + 16 * z);
-                sin[z] = pid >= 0;
-                sk[z] = p.k_scale[head_of(pid)];
-                sv[z] = p.v_scale[head_of(pid)];
-            }
-        };
         auto first_product = [&](const uint8_t* at, f16v (&S)[2]) {
             const int k0 = here(L::key_at(c, half));
 #pragma unroll
@@ -169,17 +195,23 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_tile_kernel(AttnA
                         *reinterpret_cast<const h8*>(at + 32 * y * (DP * 2) + (k0 ^ (32 * s))), Q[s], S[y], 0, 0, 0);
             }
         };
-        v4i kw[N], vw[N];
         auto step = [&](auto parity, auto last, int kt) {
             constexpr int A = decltype(parity)::value;
             constexpr bool kLast = decltype(last)::value;
             uint8_t *const keys = lds, *const values = lds + 2 * L::kKeys;
             BlockScale bs[Z];
+            {
+                const BlockScale k = block_scale(sin[A], sk[A], sv[A], p.scale);
 #pragma unroll
-            for (int z = 0; z < Z; ++z) bs[z] = block_scale(sin[z], sk[z], sv[z], p.scale);
+                for (int z = 0; z < Z; ++z) bs[z] = {lane_float(k.ks, z), lane_float(k.lv, z), lane_float(k.iv, z)};
+            }
             f16v S[2];
             first_product(keys + A * L::kKeys, S);
-            if (!kLast) fetch_scales(kt + 1);
+            if (!kLast) {
+                place_keys(keys + (A ^ 1) * L::kKeys, kw);
+                place_values(values + (A ^ 1) * L::kKeys, vw);
+                fetch(min(kt + 2, s1 - 1), parity);
+            }
             const int key0 = kt * kAttnStep;
             if (key0 < lo_most || key0 + kAttnStep > hi_least) {
                 int key = key0 + 4 * half;
@@ -210,49 +242,44 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_tile_kernel(AttnA
 #pragma unroll
                 for (int d = 0; d < DT; ++d) O[d] *= fade;
             }
-            h8 W[4];
+            // weights of 16 keys, then their part of the second product, whose matrix
+            // instructions run beside the next weights
+            const int v0 = here(L::value_at(c, half));
+            float sum = 0.0f;
 #pragma unroll
-            for (int z = 0; z < Z; ++z) {
-                float sum = 0.0f;
-                const float off = bs[z].lv - m;
+            for (int u = 0; u < 4; ++u) {
+                const BlockScale& k = bs[u * Z / 4];
+                const float off = k.lv - m;
+                h8 W;
 #pragma unroll
-                for (int e = 0; e < 32 / Z; e += 2) {
-                    const int i = z * (32 / Z) + e;
-                    const f2 w = {__builtin_amdgcn_exp2f(__builtin_fmaf(S[i / 16][i % 16], bs[z].ks, off)),
-                                  __builtin_amdgcn_exp2f(__builtin_fmaf(S[i / 16][i % 16 + 1], bs[z].ks, off))};
+                for (int e = 0; e < 8; e += 2) {
+                    const int i = 8 * u + e;
+                    const f2 w = {__builtin_amdgcn_exp2f(__builtin_fmaf(S[i / 16][i % 16], k.ks, off)),
+                                  __builtin_amdgcn_exp2f(__builtin_fmaf(S[i / 16][i % 16 + 1], k.ks, off))};
                     sum += w[0];
                     sum += w[1];
                     const h2 x = __builtin_convertvector(w, h2);
-                    W[i / 8][i % 8] = x[0];
-                    W[i / 8][i % 8 + 1] = x[1];
+                    W[e] = x[0];
+                    W[e + 1] = x[1];
                 }
-                l = __builtin_fmaf(sum, bs[z].iv, l);
-            }
-            if (!kLast) {
-                place_keys(keys + (A ^ 1) * L::kKeys, kw);
-                place_values(values + (A ^ 1) * L::kKeys, vw);
-                fetch_keys(min(kt + 2, s1 - 1), kw);
-                fetch_values(min(kt + 2, s1 - 1), vw);
-            }
-            const int v0 = here(L::value_at(c, half));
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
+                if (Z > 1 || u == 3) {
+                    l = __builtin_fmaf(sum, k.iv, l);
+                    sum = 0.0f;
+                }
 #pragma unroll
                 for (int d = 0; d < DT; ++d)
                     O[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
-                        *reinterpret_cast<const h8*>(values + A * L::kKeys + 32 * d * 128 + (v0 ^ (32 * u))), W[u], O[d],
-                        0, 0, 0);
+                        *reinterpret_cast<const h8*>(values + A * L::kKeys + 32 * d * 128 + (v0 ^ (32 * u))), W, O[d], 0, 0,
+                        0);
+            }
             if (!kLast) __syncthreads();
         };
         if (s0 < s1) {
             __syncthreads();                           // the tile before is done with the buffers
-            fetch_scales(s0);
-            fetch_keys(s0, kw);
-            fetch_values(s0, vw);
+            fetch(s0, Int<0>());
             place_keys(lds, kw);
-            fetch_keys(min(s0 + 1, s1 - 1), kw);
             place_values(lds + 2 * L::kKeys, vw);
-            fetch_values(min(s0 + 1, s1 - 1), vw);
+            fetch(min(s0 + 1, s1 - 1), Int<1>());
             __syncthreads();
             int kt = s0;
             for (; kt + 2 < s1; kt += 2) {
