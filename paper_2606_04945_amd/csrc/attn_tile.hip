@@ -51,6 +51,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_tile_kernel(AttnA
     typedef TileLds<DP> L;
     constexpr int KS = DP / 16, DT = DP / 32, N = DP / 64;   // k steps, value tiles, 16-byte loads a thread of each
     constexpr int Z = WIDE ? 1 : 4;                          // scales a step
+    constexpr int kAhead = 4;                                // operands read ahead
     const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int c = lane % 32, half = lane / 32;
     const int G = p.a.G, D = p.D, R = p.a.rows;
@@ -165,53 +166,58 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_tile_kernel(AttnA
                 sv[A] = p.v_scale[head_of(pid)];
             }
         };
-        auto place_keys = [&](uint8_t* at, const v4i (&w)[N]) {
-            const int k0 = here(L::key_at(tid / (DP / 16), tid % (DP / 16) * 2));
-#pragma unroll
-            for (int n = 0; n < N; ++n) {
+        // piece z / 2 of this thread's keys (z < 2 N) or values, its half z % 2, as halves into a buffer
+        auto place = [&](uint8_t* keys, uint8_t* values, int k0, int v0, int z) {
+            if (z < 2 * N) {
                 // 256 pieces on: a multiple of 16 rows, which share their exchange of chunks
-                const int k = k0 + 256 * 16 / DP * n * (DP * 2);
-                *reinterpret_cast<h8*>(at + k) = to_halves((uint32_t)w[n][0], (uint32_t)w[n][1]);
-                *reinterpret_cast<h8*>(at + (k ^ 16)) = to_halves((uint32_t)w[n][2], (uint32_t)w[n][3]);
-            }
-        };
-        auto place_values = [&](uint8_t* at, const v4i (&w)[N]) {
-            const int v0 = here(L::value_at(tid / 4, tid % 4 * 2));
-#pragma unroll
-            for (int n = 0; n < N; ++n) {
-                const int v = v0 + 64 * n * 128;       // 64 channels on
-                *reinterpret_cast<h8*>(at + v) = to_halves((uint32_t)w[n][0], (uint32_t)w[n][2]);
-                *reinterpret_cast<h8*>(at + (v ^ 16)) = to_halves((uint32_t)w[n][1], (uint32_t)w[n][3]);
-            }
-        };
-        auto first_product = [&](const uint8_t* at, f16v (&S)[2]) {
-            const int k0 = here(L::key_at(c, half));
-#pragma unroll
-            for (int y = 0; y < 2; ++y) {
-                S[y] = f16v{};
-#pragma unroll
-                for (int s = 0; s < KS; ++s)
-                    S[y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
-                        *reinterpret_cast<const h8*>(at + 32 * y * (DP * 2) + (k0 ^ (32 * s))), Q[s], S[y], 0, 0, 0);
+                const int n = z / 2, k = k0 + 256 * 16 / DP * n * (DP * 2);
+                *reinterpret_cast<h8*>(keys + (k ^ (z % 2 * 16))) =
+                    to_halves((uint32_t)kw[n][z % 2 * 2], (uint32_t)kw[n][z % 2 * 2 + 1]);
+            } else {
+                const int n = z / 2 - N, v = v0 + 64 * n * 128;      // 64 channels on
+                *reinterpret_cast<h8*>(values + (v ^ (z % 2 * 16))) =
+                    to_halves((uint32_t)vw[n][z % 2], (uint32_t)vw[n][z % 2 + 2]);
             }
         };
         auto step = [&](auto parity, auto last, int kt) {
             constexpr int A = decltype(parity)::value;
             constexpr bool kLast = decltype(last)::value;
-            uint8_t *const keys = lds, *const values = lds + 2 * L::kKeys;
+            uint8_t *const keys = lds + A * L::kKeys, *const values = lds + (2 + A) * L::kKeys;
             BlockScale bs[Z];
             {
                 const BlockScale k = block_scale(sin[A], sk[A], sv[A], p.scale);
 #pragma unroll
                 for (int z = 0; z < Z; ++z) bs[z] = {lane_float(k.ks, z), lane_float(k.lv, z), lane_float(k.iv, z)};
             }
+            // First product, two tiles of 32 keys.  Operands are read kAhead instructions ahead;
+            // the second tile's run beside the next step's codes becoming halves.  Barriers to
+            // the scheduler hold this order: left to itself it reads an operand, waits and multiplies.
             f16v S[2];
-            first_product(keys + A * L::kKeys, S);
-            if (!kLast) {
-                place_keys(keys + (A ^ 1) * L::kKeys, kw);
-                place_values(values + (A ^ 1) * L::kKeys, vw);
-                fetch(min(kt + 2, s1 - 1), parity);
+            h8 K[kAhead];
+            const int k0 = here(L::key_at(c, half));
+            auto key_operand = [&](int i) {
+                return *reinterpret_cast<const h8*>(keys + i / KS * 32 * (DP * 2) + (k0 ^ (32 * (i % KS))));
+            };
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) K[i] = key_operand(i);
+            __builtin_amdgcn_sched_barrier(0);
+            const int kp = here(L::key_at(tid / (DP / 16), tid % (DP / 16) * 2));
+            const int vp = here(L::value_at(tid / 4, tid % 4 * 2));
+#pragma unroll
+            for (int i = 0; i < 2 * KS; ++i) {
+                S[i / KS] = __builtin_amdgcn_mfma_f32_32x32x16_f16(K[i % kAhead], Q[i % KS], i % KS ? S[i / KS] : f16v{},
+                                                                  0, 0, 0);
+                if (i + kAhead < 2 * KS) K[i % kAhead] = key_operand(i + kAhead);
+                if (!kLast && i >= KS) place(lds + (A ^ 1) * L::kKeys, lds + (2 + (A ^ 1)) * L::kKeys, kp, vp, i - KS);
+                __builtin_amdgcn_sched_barrier(0);
             }
+            if (!kLast) fetch(min(kt + 2, s1 - 1), parity);
+            h8 V[2][DT];
+            const int v0 = here(L::value_at(c, half));
+#pragma unroll
+            for (int d = 0; d < DT; ++d) V[0][d] = *reinterpret_cast<const h8*>(values + 32 * d * 128 + v0);
+            __builtin_amdgcn_sched_barrier(0);
+
             const int key0 = kt * kAttnStep;
             if (key0 < lo_most || key0 + kAttnStep > hi_least) {
                 int key = key0 + 4 * half;
@@ -242,43 +248,53 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_tile_kernel(AttnA
 #pragma unroll
                 for (int d = 0; d < DT; ++d) O[d] *= fade;
             }
-            // weights of 16 keys, then their part of the second product, whose matrix
-            // instructions run beside the next weights
-            const int v0 = here(L::value_at(c, half));
+            // Second product, 16 keys at a time: the next 16 weights and operands beside the
+            // instructions of these
             float sum = 0.0f;
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
+            h8 W[2];
+            auto weights = [&](int u, int e) {         // two of them
                 const BlockScale& k = bs[u * Z / 4];
                 const float off = k.lv - m;
-                h8 W;
-#pragma unroll
-                for (int e = 0; e < 8; e += 2) {
-                    const int i = 8 * u + e;
-                    const f2 w = {__builtin_amdgcn_exp2f(__builtin_fmaf(S[i / 16][i % 16], k.ks, off)),
-                                  __builtin_amdgcn_exp2f(__builtin_fmaf(S[i / 16][i % 16 + 1], k.ks, off))};
-                    sum += w[0];
-                    sum += w[1];
-                    const h2 x = __builtin_convertvector(w, h2);
-                    W[e] = x[0];
-                    W[e + 1] = x[1];
-                }
-                if (Z > 1 || u == 3) {
+                const int i = 8 * u + e;
+                const f2 w = {__builtin_amdgcn_exp2f(__builtin_fmaf(S[i / 16][i % 16], k.ks, off)),
+                              __builtin_amdgcn_exp2f(__builtin_fmaf(S[i / 16][i % 16 + 1], k.ks, off))};
+                sum += w[0];
+                sum += w[1];
+                const h2 x = __builtin_convertvector(w, h2);
+                W[u % 2][e] = x[0];
+                W[u % 2][e + 1] = x[1];
+                if (e == 6 && (Z > 1 || u == 3)) {
                     l = __builtin_fmaf(sum, k.iv, l);
                     sum = 0.0f;
                 }
+            };
 #pragma unroll
-                for (int d = 0; d < DT; ++d)
-                    O[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
-                        *reinterpret_cast<const h8*>(values + A * L::kKeys + 32 * d * 128 + (v0 ^ (32 * u))), W, O[d], 0, 0,
-                        0);
-            }
+            for (int e = 0; e < 8; e += 2) weights(0, e);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int d = 0; d < DT; ++d) {
+                    if (u < 3)
+                        V[(u + 1) % 2][d] =
+                            *reinterpret_cast<const h8*>(values + 32 * d * 128 + (v0 ^ (32 * (u + 1))));
+                    O[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(V[u % 2][d], W[u % 2], O[d], 0, 0, 0);
+                    if (u < 3) {
+#pragma unroll
+                        for (int e = 0; e < 8; e += 2)
+                            if (e * DT / 8 == d) weights(u + 1, e);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
             if (!kLast) __syncthreads();
         };
         if (s0 < s1) {
             __syncthreads();                           // the tile before is done with the buffers
             fetch(s0, Int<0>());
-            place_keys(lds, kw);
-            place_values(lds + 2 * L::kKeys, vw);
+#pragma unroll
+            for (int z = 0; z < 4 * N; ++z)
+                place(lds, lds + 2 * L::kKeys, L::key_at(tid / (DP / 16), tid % (DP / 16) * 2),
+                      L::value_at(tid / 4, tid % 4 * 2), z);
             fetch(min(s0 + 1, s1 - 1), Int<1>());
             __syncthreads();
             int kt = s0;
