@@ -41,6 +41,9 @@ SHAPES = [
     (1, 8, 64, 32), (1, 4096, 4096, 128), (1, 24, 192, 64), (3, 40, 320, 32), (16, 520, 1024, 128),
     (17, 264, 1152, 384), (5, 3584, 18944, 64), (33, 72, 2048, 1024), (64, 136, 640, 640), (65, 16, 256, 128),
     (130, 1032, 576, 32), (2, 12288, 512, 64), (31, 16392, 128, 128),
+    # every number of output groups a workgroup can have, ragged, at each kind of group
+    (1, 24576, 256, 32), (16, 37888, 192, 64), (9, 24584, 384, 128), (1, 16392, 512, 512), (12, 20488, 320, 32),
+    (16, 61448, 128, 64), (40, 16408, 256, 128), (17, 8200, 192, 64), (64, 12296, 128, 32), (3, 8168, 448, 64),
 ]
 
 
