@@ -70,7 +70,7 @@ __global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(AttnArgs p, int
         float m = kUnseen, l = 0.0f;
         f4 O{0, 0, 0, 0};
         if (mine) {
-            constexpr int U = 4;                  // results requested together
+            constexpr int U = 8;                  // results requested together
             for (int j0 = gi % each; j0 < n; j0 += U * each) {
                 float mj[U], lj[U];
                 f4 Oj[U];

@@ -154,7 +154,7 @@ SQ_HD bool attn_direct(const AttnShape& a, int64_t total, int64_t most) {
 // Which kernel a call takes, by what the host knows: rows and the length that a page
 // table row can hold, not the lengths themselves.
 //   up to 16 rows a sequence and key head, on average: tiles of 16
-//   up to 64: tiles of 32
+//   up to 64: tiles of 32, of 16 for heads above 128
 //   more: tiles of 128
 // The first two read with single waves (four or eight of a workgroup, one workgroup a
 // CU), the last with workgroups of four waves, two a CU.
@@ -172,7 +172,7 @@ inline AttnShape attn_shape(int T, int B, int Hq, int heads, int D, int max_len,
     const int G = Hq / heads;
     const int64_t rows = (int64_t)T * G;
     AttnShape a{T, B, heads, G, max_len, causal, window, 0, kAttnCus, 0, 1024};
-    a.rows = rows <= (int64_t)16 * B ? 16 : rows <= (int64_t)64 * B ? 32 : 128;
+    a.rows = rows > (int64_t)64 * B ? 128 : rows > (int64_t)16 * B && D <= 128 ? 32 : 16;
     if (a.rows == 128) a.groups = a.workers = D <= 128 ? 2 * kAttnCus : kAttnCus;
     else a.workers = a.groups * attn_waves(a.rows, D);
     return a;

@@ -55,128 +55,138 @@ struct WaveRows {
         }
     }
 
-    // Steps first, first + stride, ... below end.  What the next step reads is
-    // requested as soon as the registers of this one's are free: its keys before this
-    // step's softmax, its values after the second product, its pages a step earlier.
+    // What a step reads, a lane's part: the pages of its key row (group c / 4 of the step)
+    // and of its lane group's keys, codes and scales.  Every load is issued on every step
+    // (addresses are kept inside instead), so that waiting for some leaves the others in
+    // flight.
+    struct Reads {
+        int kp, vp;                               // pages, -1: none
+        v4i k[4][P], v[DT];
+        float ks, vs;
+    };
+    __device__ __forceinline__ void pages(const AttnArgs& p, const Seq& s, const int32_t* table, int kt, int c, int g,
+                                          int& kp, int& vp) const {
+        const int ka = kt * kAttnStep + 16 * (c / 4), va = kt * kAttnStep + 16 * g;
+        const int k = table[min(ka, s.len - 1) >> p.shift], v = table[min(va, s.len - 1) >> p.shift];
+        kp = ka < s.len && (uint32_t)k < (uint32_t)p.pages ? k : -1;
+        vp = va < s.len && (uint32_t)v < (uint32_t)p.pages ? v : -1;
+    }
+    __device__ __forceinline__ void keys(const AttnArgs& p, int h, int kt, int c, int g, Reads& r) const {
+        const int ka = kt * kAttnStep + 16 * (c / 4);
+        const int64_t ph = r.kp >= 0 ? (int64_t)r.kp * p.a.heads + h : h;
+        const int8_t* at = p.k + (ph * p.page + (ka & (p.page - 1)) + c % 4) * p.D;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int z = 0; z < P; ++z)           // past the channels: others again, which meet zero queries
+                r.k[e][z] = *reinterpret_cast<const v4i*>(at + 4 * e * p.D + min(64 * z + 16 * g, p.D - 16));
+    }
+    __device__ __forceinline__ void values(const AttnArgs& p, int h, int kt, int c, int g, Reads& r) const {
+        const int64_t ph = r.vp >= 0 ? (int64_t)r.vp * p.a.heads + h : h;
+        const int8_t* at = p.v + ph * p.page * p.D + ((kt * kAttnStep + 16 * g) & (p.page - 1));
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+            r.v[d] = *reinterpret_cast<const v4i*>(at + min(16 * d + c, p.D - 1) * p.page);
+    }
+    __device__ __forceinline__ void scales(const AttnArgs& p, int h, Reads& r) const {
+        const int64_t ph = r.vp >= 0 ? (int64_t)r.vp * p.a.heads + h : h;
+        r.ks = p.k_scale[ph];
+        r.vs = p.v_scale[ph];
+    }
+
+    // Steps first, first + stride, ... below end.  What the next step reads is requested as
+    // soon as the registers of this one's are free: its keys before this step's softmax,
+    // its values after the second product, its pages a step earlier.
     __device__ __forceinline__ void pass(const AttnArgs& p, const Seq& s, int b, int h, int first, int end, int stride,
                                          int c, int g) {
-        if (first >= end) return;
-        const int32_t* table = p.table + (int64_t)b * p.max_pages;
-        const int D = p.D;
-        int kp, vp, kn, vn;                       // pages of this lane's key row and of its lane group, now and next
-        auto pages = [&](int kt, int& a, int& z) {
-            const int ka = kt * kAttnStep + 16 * (c / 4), va = kt * kAttnStep + 16 * g;
-            a = ka < s.len ? table[ka >> p.shift] : -1;
-            z = va < s.len ? table[va >> p.shift] : -1;
-        };
-        v4i kw[4][P], vw[DT];
-        float ks, vs;
-        auto keys = [&](int kt, int pid) {
-            const int ka = kt * kAttnStep + 16 * (c / 4);
-            const int64_t ph = (uint32_t)pid < (uint32_t)p.pages ? (int64_t)pid * p.a.heads + h : h;
-            const int8_t* at = p.k + (ph * p.page + (ka & (p.page - 1)) + c % 4) * D + 16 * g;
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-#pragma unroll
-                for (int z = 0; z < P; ++z)
-                    kw[e][z] = 64 * z + 16 * g < D ? *reinterpret_cast<const v4i*>(at + 4 * e * D + 64 * z)
-                                                   : v4i{0, 0, 0, 0};
-        };
-        auto values = [&](int kt, int pid) {
-            const int va = kt * kAttnStep + 16 * g;
-            const int64_t ph = (uint32_t)pid < (uint32_t)p.pages ? (int64_t)pid * p.a.heads + h : h;
-            const int8_t* at = p.v + ph * p.page * D + (va & (p.page - 1));
-#pragma unroll
-            for (int d = 0; d < DT; ++d) vw[d] = *reinterpret_cast<const v4i*>(at + min(16 * d + c, D - 1) * p.page);
-        };
-        auto scales = [&](int pid) {
-            const int64_t ph = (uint32_t)pid < (uint32_t)p.pages ? (int64_t)pid * p.a.heads + h : h;
-            ks = p.k_scale[ph];
-            vs = p.v_scale[ph];
-        };
-        pages(first, kp, vp);
-        kn = vn = -1;
-        if (first + stride < end) pages(first + stride, kn, vn);
-        keys(first, kp);
-        scales(vp);
-        values(first, vp);
-        for (int kt = first; kt < end; kt += stride) {
-            const bool more = kt + stride < end;
-            const int key0 = kt * kAttnStep, va = key0 + 16 * g;
-            const bool vin = (uint32_t)vp < (uint32_t)p.pages;
-            f4 S[QT][4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-#pragma unroll
-                for (int y = 0; y < QT; ++y) S[y][e] = f4{0, 0, 0, 0};
-#pragma unroll
-                for (int z = 0; z < 2 * P; ++z) {
-                    const v4i w = kw[e][z / 2];
-                    const h8 k = to_halves((uint32_t)w[2 * (z % 2)], (uint32_t)w[2 * (z % 2) + 1]);
-#pragma unroll
-                    for (int y = 0; y < QT; ++y)
-                        S[y][e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, Q[y][z], S[y][e], 0, 0, 0);
-                }
-            }
-            const float ks0 = ks, vs0 = vs;
-            if (more) {
-                kp = kn, vp = vn;
-                keys(kt + stride, kp);
-                scales(vp);
-                kn = vn = -1;
-                if (kt + 2 * stride < end) pages(kt + 2 * stride, kn, vn);
-            }
-            h8 W[QT][2];
-#pragma unroll
-            for (int y = 0; y < QT; ++y) {
-                const BlockScale bs = block_scale(vin, ks0, vs0, p.scale);
-                if (!__all(key0 >= lo[y] && key0 + kAttnStep <= hi[y])) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int key = va + 4 * e + i;
-                            if (key < lo[y] || key >= hi[y]) S[y][e][i] = kHidden;
-                        }
-                }
-                float mx = S[y][0][0];
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) mx = fmaxf(mx, S[y][e][i]);
-                mx = fmaxf(m[y], groups_max(__builtin_fmaf(mx, bs.ks, bs.lv)));
-                const float fade = __builtin_amdgcn_exp2f(m[y] - mx), off = bs.lv - mx;
-                m[y] = mx;
-                float sum = 0.0f;
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-#pragma unroll
-                    for (int i = 0; i < 4; i += 2) {
-                        const f2 w = {__builtin_amdgcn_exp2f(__builtin_fmaf(S[y][e][i], bs.ks, off)),
-                                      __builtin_amdgcn_exp2f(__builtin_fmaf(S[y][e][i + 1], bs.ks, off))};
-                        sum += w[0];
-                        sum += w[1];
-                        const h2 x = __builtin_convertvector(w, h2);
-                        W[y][e / 2][4 * (e % 2) + i] = x[0];
-                        W[y][e / 2][4 * (e % 2) + i + 1] = x[1];
-                    }
-                l[y] = __builtin_fmaf(sum, bs.iv, l[y] * fade);
-#pragma unroll
-                for (int d = 0; d < DT; ++d) O[y][d] *= fade;
-            }
-#pragma unroll
-            for (int d = 0; d < DT; ++d)
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const h8 v = to_halves((uint32_t)vw[d][2 * u], (uint32_t)vw[d][2 * u + 1]);
-#pragma unroll
-                    for (int y = 0; y < QT; ++y)
-                        O[y][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, W[y][u], O[y][d], 0, 0, 0);
-                }
-            if (more) values(kt + stride, vp);
+        if (first < end) {
+            const int32_t* table = p.table + (int64_t)b * p.max_pages;
+            Reads r;
+            pages(p, s, table, first, c, g, r.kp, r.vp);
+            int kn, vn;                           // pages of the next step
+            pages(p, s, table, first + stride, c, g, kn, vn);
+            keys(p, h, first, c, g, r);
+            scales(p, h, r);
+            values(p, h, first, c, g, r);
+            int kt = first;
+            for (; kt + stride < end; kt += stride) step<true>(p, s, table, h, kt, stride, c, g, r, kn, vn);
+            step<false>(p, s, table, h, kt, stride, c, g, r, kn, vn);
         }
 #pragma unroll
         for (int y = 0; y < QT; ++y) l[y] = groups_sum(l[y]);
+    }
+
+    template <bool MORE>
+    __device__ __forceinline__ void step(const AttnArgs& p, const Seq& s, const int32_t* table, int h, int kt, int stride,
+                                         int c, int g, Reads& r, int& kn, int& vn) {
+        const int key0 = kt * kAttnStep, va = key0 + 16 * g;
+        const BlockScale bs = block_scale(r.vp >= 0, r.ks, r.vs, p.scale);
+        f4 S[QT][4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+#pragma unroll
+            for (int y = 0; y < QT; ++y) S[y][e] = f4{0, 0, 0, 0};
+#pragma unroll
+            for (int z = 0; z < 2 * P; ++z) {
+                const v4i w = r.k[e][z / 2];
+                const h8 k = to_halves((uint32_t)w[2 * (z % 2)], (uint32_t)w[2 * (z % 2) + 1]);
+#pragma unroll
+                for (int y = 0; y < QT; ++y) S[y][e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, Q[y][z], S[y][e], 0, 0, 0);
+            }
+        }
+        if (MORE) {
+            r.kp = kn, r.vp = vn;
+            keys(p, h, kt + stride, c, g, r);
+            scales(p, h, r);
+            pages(p, s, table, kt + 2 * stride, c, g, kn, vn);
+        }
+        h8 W[QT][2];
+#pragma unroll
+        for (int y = 0; y < QT; ++y) {
+            if (!__all(key0 >= lo[y] && key0 + kAttnStep <= hi[y])) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int key = va + 4 * e + i;
+                        if (key < lo[y] || key >= hi[y]) S[y][e][i] = kHidden;
+                    }
+            }
+            float mx = S[y][0][0];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) mx = fmaxf(mx, S[y][e][i]);
+            mx = fmaxf(m[y], groups_max(__builtin_fmaf(mx, bs.ks, bs.lv)));
+            const float fade = __builtin_amdgcn_exp2f(m[y] - mx), off = bs.lv - mx;
+            m[y] = mx;
+            float sum = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int i = 0; i < 4; i += 2) {
+                    const f2 w = {__builtin_amdgcn_exp2f(__builtin_fmaf(S[y][e][i], bs.ks, off)),
+                                  __builtin_amdgcn_exp2f(__builtin_fmaf(S[y][e][i + 1], bs.ks, off))};
+                    sum += w[0];
+                    sum += w[1];
+                    const h2 x = __builtin_convertvector(w, h2);
+                    W[y][e / 2][4 * (e % 2) + i] = x[0];
+                    W[y][e / 2][4 * (e % 2) + i + 1] = x[1];
+                }
+            l[y] = __builtin_fmaf(sum, bs.iv, l[y] * fade);
+#pragma unroll
+            for (int d = 0; d < DT; ++d) O[y][d] *= fade;
+        }
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const h8 v = to_halves((uint32_t)r.v[d][2 * u], (uint32_t)r.v[d][2 * u + 1]);
+#pragma unroll
+                for (int y = 0; y < QT; ++y)
+                    O[y][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, W[y][u], O[y][d], 0, 0, 0);
+            }
+        if (MORE) values(p, h, kt + stride, c, g, r);
     }
 
     __device__ __forceinline__ void store(const AttnArgs& p, int g) const {
@@ -296,15 +306,13 @@ hipError_t launch(const AttnArgs& p, hipStream_t st) {
     return hipGetLastError();
 }
 
-template <int DP>
-hipError_t launch_rows(const AttnArgs& p, hipStream_t st) {
-    return p.a.rows == 16 ? launch<DP, 1>(p, st) : launch<DP, 2>(p, st);
-}
-
 }  // namespace
 
 hipError_t launch_attn_wave(const AttnArgs& p, hipStream_t st) {
-    return p.D <= 64 ? launch_rows<64>(p, st) : p.D <= 128 ? launch_rows<128>(p, st) : launch_rows<256>(p, st);
+    const bool two = p.a.rows == 32;
+    if (p.D <= 64) return two ? launch<64, 2>(p, st) : launch<64, 1>(p, st);
+    if (p.D <= 128) return two ? launch<128, 2>(p, st) : launch<128, 1>(p, st);
+    return two ? hipErrorInvalidConfiguration : launch<256, 1>(p, st);
 }
 
 }  // namespace sq

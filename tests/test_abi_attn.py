@@ -126,9 +126,9 @@ def test_attention(lib):
         assert attn(lib, **kw) == L.SQ_ERR_ALIGN, kw
     assert lib.attn_kv8(FAKE, 256, 64, None, FAKE, FAKE, FAKE, 4, 2, 3, 4, 1, 0, 0.1, FAKE, None, FAKE, 1 << 30,
                         None) == L.SQ_ERR_NULL
-    need = lib.sq_attn_kv8_workspace_bytes(4, 2, 4, 2, 64, 192)
+    need = lib.sq_attn_kv8_workspace_bytes(4, 2, 4, 2, 64, 640 * 64)
     assert need > 0
-    assert attn(lib, wsb=need - 1) == L.SQ_ERR_WORKSPACE and attn(lib, ws=None) == L.SQ_ERR_WORKSPACE
+    assert attn(lib, mp=640, wsb=need - 1) == L.SQ_ERR_WORKSPACE and attn(lib, mp=640, ws=None) == L.SQ_ERR_WORKSPACE
     assert attn(lib, T=0, Q=None) == L.SQ_OK and attn(lib, B=0, O=None) == L.SQ_OK
     for a in ((0, 1, 4, 2, 64, 192), (1, 0, 4, 2, 64, 192), (1, 1, 3, 2, 64, 192), (1, 1, 4, 0, 64, 192),
               (1, 1, 4, 2, 64, -1), (1, 1, 0, 2, 64, 100)):
