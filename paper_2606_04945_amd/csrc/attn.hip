@@ -5,118 +5,86 @@
 namespace sq {
 namespace {
 
-// Joins the partial results of a tile: out = sum_i 2^(m_i - M) O_i / sum_i 2^(m_i - M) l_i.
-// A workgroup has `share` rows of one tile.  A group of `vecs` threads has a row,
-// four channels a thread; where the results are many, several groups share a row's,
-// and meet in LDS in order.  Which worker ended first changes nothing.
-constexpr int kJoinThreads = 256, kJoinPlaces = 2048, kJoinAtOnce = 256 * 8;
-__global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(AttnArgs p, int share) {
-    __shared__ int places[kJoinPlaces];
-    __shared__ int counts[kJoinThreads / kWave];
-    __shared__ float ml[2 * kJoinThreads];
+// Joins the partial results of the tiles that workers share:
+//   out = sum_i 2^(m_i - M) O_i / sum_i 2^(m_i - M) l_i.
+// A workgroup looks at `each` workers' records and joins `share` rows of the tiles it
+// finds there.  A group of D / 4 threads has a row, four channels a thread; where a tile
+// has more groups than rows, several share a row's results and meet in LDS in order.
+// Which worker ended first changes nothing.
+constexpr int kJoinThreads = 256, kJoinGroups = 64;    // at most: heads of 16
+__global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(AttnArgs p, int each, int share) {
+    __shared__ float ml[2 * kJoinGroups];
     __shared__ f4 part[kJoinThreads];
-    const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
-    const int R = p.a.rows, D = p.D, G = p.a.G;
-    const int64_t item = blockIdx.x / p.a.heads;
-    const int h = blockIdx.x % p.a.heads;
-    const Group first = load_group(p, 0, lane);
-    const Survey all = survey(p, first, lane);
-    if (all.direct) return;
-    const Listed at_item = find_listed<true>(p, item, first, lane);
-    const AttnSeq q = at_item.q;
-    const int64_t r64 = item - list_start(q.s.t0, at_item.b, G, R, 1);
-    if (r64 < 0 || r64 >= q.tiles) return;
-    const int r = (int)r64, row0 = blockIdx.y * share;
-    const int rows = min(min(R, row0 + share), q.s.n * G - r * R);
-    if (row0 >= rows) return;
-    const AttnSteps steps = attn_steps(p.a, q.s, r);
-    if (steps.count <= 1) return;                 // never split
-    const int64_t before = at_item.before;
-    const AttnCut cut = attn_cut_work(all.total, p.a.workers);
-    const int64_t from = before + h * q.weight + attn_before(q, r), weight = q.base + q.slope * r;
-    const int w0 = attn_worker(cut, from), w1 = attn_worker(cut, from + weight - 1);
-    if (w0 == w1) return;
-    int n = 0;                                    // results, in the workers' order
-    for (int wb = w0; wb <= w1; wb += kJoinThreads) {
-        const int w = wb + tid;
-        int place = -1;
-        bool alone = false;
-        if (w <= w1) {
-            const int64_t x0 = attn_start(cut, w) - from, x1 = min(attn_start(cut, w + 1) - from, weight);
-            const int k0 = attn_cut(x0, weight, steps.count), k1 = attn_cut(x1, weight, steps.count);
-            alone = k1 - k0 == steps.count;
-            if (k1 > k0) place = attn_place(w, x0 > 0);
-        }
-        if (__syncthreads_or(alone)) return;      // one worker had every step and wrote the rows
-        const uint64_t some = __ballot(place >= 0);
-        if (lane == 0) counts[wave] = __popcll(some);
-        __syncthreads();
-        int base = n;
-#pragma unroll
-        for (int v = 0; v < kJoinThreads / kWave; ++v) {
-            if (v < wave) base += counts[v];
-            n += counts[v];
-        }
-        if (place >= 0) places[base + __popcll(some & ((1ull << lane) - 1))] = place;
-    }
-    __syncthreads();
-    const int vecs = D / 4, groups = kJoinThreads / vecs;
-    const int each = min(n, max(1, groups / (rows - row0)));      // groups of threads to a row
+    const int tid = threadIdx.x, R = p.a.rows, D = p.D, G = p.a.G;
+    const int vecs = D / 4, groups = kJoinThreads / vecs, gi = tid / vecs, v = tid % vecs;
+    const int first = blockIdx.x * each, row0 = blockIdx.y * share;
     const int64_t size = attn_place_floats(R, D);
-    const int gi = tid / vecs, v = tid % vecs;
-    for (int first = row0; first < rows; first += groups / each) {
-        const int row = first + gi / each;
-        const bool mine = gi < groups && row < rows;
-        float m = kUnseen, l = 0.0f;
-        f4 O{0, 0, 0, 0};
-        if (mine) {
-            constexpr int U = 8;                  // results requested together
-            for (int j0 = gi % each; j0 < n; j0 += U * each) {
-                float mj[U], lj[U];
-                f4 Oj[U];
+    // a wave's lanes look at the records together
+    const int lane = tid % kWave, mine = first + lane;
+    const int last = lane < each && mine < p.a.workers ? p.records[mine].last : -1;
+    for (uint64_t found = __ballot(last >= 0); found; found &= found - 1) {
+        const int w0 = first + __builtin_ctzll(found), n = __builtin_amdgcn_readlane(last, w0 - first) - w0 + 1;
+        const AttnRecord t = p.records[w0];
+        const int rows = min(min(R, row0 + share), t.rows - t.row0);
+        if (row0 >= rows) continue;
+        const int per = min(n, max(1, groups / (rows - row0)));          // groups of threads to a row
+        for (int r0 = row0; r0 < rows; r0 += groups / per) {
+            const int row = r0 + gi / per;
+            const bool in = gi < groups / per * per && row < rows;
+            float m = kNone, l = 0.0f;
+            f4 O{0, 0, 0, 0};
+            if (in) {
+                constexpr int U = 4;                   // results requested together
+                for (int j0 = gi % per; j0 < n; j0 += U * per) {
+                    float mj[U], lj[U];
+                    f4 Oj[U];
 #pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    const int j = j0 + u * each;
-                    const float* ws = p.ws + places[min(j, n - 1)] * size;
-                    mj[u] = j < n ? ws[R * D + row] : kNone;
-                    lj[u] = ws[R * D + R + row];
-                    Oj[u] = *reinterpret_cast<const f4*>(ws + row * D + 4 * v);
+                    for (int u = 0; u < U; ++u) {
+                        const int j = j0 + u * per, w = w0 + min(j, n - 1);
+                        const float* ws = p.places + attn_place(w, w > w0) * size;
+                        mj[u] = j < n ? ws[R * D + row] : kNone;
+                        lj[u] = ws[R * D + R + row];
+                        Oj[u] = *reinterpret_cast<const f4*>(ws + row * D + 4 * v);
+                    }
+                    float mn = m;
+#pragma unroll
+                    for (int u = 0; u < U; ++u) mn = fmaxf(mn, mj[u]);
+                    const float ms = fmaxf(mn, kUnseen);                 // -inf: nothing yet
+                    const float f = __builtin_amdgcn_exp2f(m - ms);
+                    O *= f;
+                    l *= f;
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        // a place without a maximum holds no sums either
+                        const bool some = mj[u] != kNone;
+                        const float fu = __builtin_amdgcn_exp2f(mj[u] - ms);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) O[i] = some ? __builtin_fmaf(Oj[u][i], fu, O[i]) : O[i];
+                        l = some ? __builtin_fmaf(lj[u], fu, l) : l;
+                    }
+                    m = mn;
                 }
-                float mn = m;
-#pragma unroll
-                for (int u = 0; u < U; ++u) mn = fmaxf(mn, mj[u]);
-                const float f = __builtin_amdgcn_exp2f(m - mn);
-                O *= f;
-                l *= f;
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    const float fu = __builtin_amdgcn_exp2f(mj[u] - mn);
-                    O += Oj[u] * fu;
-                    l = __builtin_fmaf(lj[u], fu, l);
-                }
-                m = mn;
             }
-        }
-        if (each > 1) {
-            __syncthreads();
-            part[tid] = O;
-            ml[tid] = m, ml[kJoinThreads + tid] = l;
-            __syncthreads();
-            if (!mine || gi % each) continue;
-            for (int z = 1; z < each; ++z) {
-                const int o = tid + z * vecs;
-                const float mn = fmaxf(m, ml[o]);
-                const float f = __builtin_amdgcn_exp2f(m - mn), fz = __builtin_amdgcn_exp2f(ml[o] - mn);
-                O = O * f + part[o] * fz;
-                l = l * f + ml[kJoinThreads + o] * fz;
-                m = mn;
+            if (per > 1) {
+                __syncthreads();
+                part[tid] = O;
+                if (v == 0 && gi < groups) ml[gi] = m, ml[kJoinGroups + gi] = l;
+                __syncthreads();
+                if (in && gi % per == 0)
+                    for (int z = 1; z < per; ++z) {
+                        const float mz = ml[gi + z], mn = fmaxf(m, mz), ms = fmaxf(mn, kUnseen);
+                        const float f = __builtin_amdgcn_exp2f(m - ms), fz = __builtin_amdgcn_exp2f(mz - ms);
+                        O = O * f + part[tid + z * vecs] * fz;
+                        l = l * f + ml[kJoinGroups + gi + z] * fz;
+                        m = mn;
+                    }
             }
+            if (!in || gi % per || m == kNone) continue;      // no maximum: one worker wrote the row
+            const int at = t.row0 + row;
+            const int64_t o = (int64_t)(t.t0 + at / G) * p.a.heads * G + t.h * G + at % G;
+            store_result(p.O + o * D + 4 * v, O, l > 0.0f ? 1.0f / l : 0.0f);
+            if (p.lse && v == 0) p.lse[o] = result_lse(m, l);
         }
-        if (!mine) continue;
-        const int at = r * R + row;
-        const int64_t o = (int64_t)(q.s.t0 + at / G) * p.a.heads * G + h * G + at % G;
-        store_result(p.O + o * D + 4 * v, O, l > 0.0f ? 1.0f / l : 0.0f);
-        if (p.lse && v == 0) p.lse[o] = result_lse(m, l);
     }
 }
 
@@ -124,7 +92,7 @@ __global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(AttnArgs p, int
 
 size_t attn_workspace_bytes(int T, int B, int Hq, int heads, int D, int max_len) {
     const AttnShape a = attn_shape(T, B, Hq, heads, D, max_len, true, 0);
-    return attn_always_direct(a) ? 0 : (size_t)a.workers * 2 * attn_place_floats(a.rows, D) * sizeof(float);
+    return attn_always_direct(a) ? 0 : (size_t)attn_workspace(a, D);
 }
 
 hipError_t launch_attn(const uint16_t* Q, int64_t q_token, int64_t q_head, const int8_t* k, const int8_t* v,
@@ -132,17 +100,16 @@ hipError_t launch_attn(const uint16_t* Q, int64_t q_token, int64_t q_head, const
                        const int32_t* cu, const int32_t* lens, const int32_t* table, int T, int B, int max_pages, int Hq,
                        bool causal, int window, float scale, uint16_t* O, float* lse, void* ws, hipStream_t st) {
     const AttnShape a = attn_shape(T, B, Hq, heads, D, max_pages * page, causal, window);
+    AttnRecord* records = static_cast<AttnRecord*>(ws);
     const AttnArgs p{a, Q, q_token, q_head, k, v, k_scale, v_scale, pages, page, __builtin_ctz((unsigned)page), D,
                      cu, lens, table, max_pages, fabsf(scale) * kLog2e, scale < 0.0f ? 0x80008000u : 0u, O, lse,
-                     static_cast<float*>(ws)};
+                     records, reinterpret_cast<float*>(records + a.workers)};
     const hipError_t e = a.rows > 32 ? launch_attn_tile(p, st) : launch_attn_wave(p, st);
     if (e != hipSuccess || attn_always_direct(a)) return e;
-    // rows a joining workgroup has: fewer while the workgroups still run all at once
-    const int64_t tiles = attn_tile_slots(a);
-    int share = a.rows;
-    while (share > 1 && tiles * (a.rows / share) < kJoinAtOnce) share /= 2;
-    hipLaunchKernelGGL(attn_join_kernel, dim3((unsigned)tiles, (unsigned)(a.rows / share)), dim3(kJoinThreads), 0,
-                       st, p, share);
+    // about 2048 workgroups: few long lists of results (a row each) or many short ones
+    const int each = a.rows > 32 ? 1 : 16, share = a.rows > 32 ? 32 : 1;
+    hipLaunchKernelGGL(attn_join_kernel, dim3((unsigned)((a.workers + each - 1) / each), (unsigned)(a.rows / share)),
+                       dim3(kJoinThreads), 0, st, p, each, share);
     return hipGetLastError();
 }
 

@@ -34,7 +34,8 @@ struct AttnArgs {
     uint32_t flip;                  // sign bits of a pair of halves where the scale is negative
     uint16_t* O;
     float* lse;
-    float* ws;
+    AttnRecord* records;            // of the workspace, and its places
+    float* places;
 };
 
 hipError_t launch_attn_wave(const AttnArgs& p, hipStream_t st);
@@ -136,11 +137,12 @@ __device__ __forceinline__ Survey survey(const AttnArgs& p, const Group& first, 
 struct Share {
     int64_t at, end, before;
     int b;
+    AttnCut cut;
 };
 __device__ __forceinline__ Share find_share(const AttnArgs& p, int64_t total, const Group& first, int worker,
                                             int lane) {
     const AttnCut cut = attn_cut_work(total, p.a.workers);
-    Share s{attn_start(cut, worker), attn_start(cut, worker + 1), 0, p.a.B};
+    Share s{attn_start(cut, worker), attn_start(cut, worker + 1), 0, p.a.B, cut};
     for (int b0 = 0; b0 < p.a.B; b0 += kWave) {
         const int64_t w = group_seq(p, b0 ? load_group(p, b0, lane) : first).weight, upto = wave_scan(w);
         const uint64_t past = __ballot(s.before + upto * p.a.heads > s.at);
@@ -156,17 +158,13 @@ __device__ __forceinline__ Share find_share(const AttnArgs& p, int64_t total, co
 }
 
 // The sequence whose list of tiles holds place `item`: the last whose list starts
-// at or before it (list starts do not decrease); and the weight of those before it,
-// where asked.
+// at or before it (list starts do not decrease).
 struct Listed {
     int b;
     AttnSeq q;
-    int64_t before;
 };
-template <bool WEIGHTS>
 __device__ __forceinline__ Listed find_listed(const AttnArgs& p, int64_t item, const Group& first, int lane) {
     Listed r{};
-    int64_t done = 0;
     Group g = first;
     for (int b0 = 0;;) {
         const bool at = b0 + lane < p.a.B && list_start(min(max(g.c0, 0), p.a.T), b0 + lane, p.a.G, p.a.rows, 1) <= item;
@@ -174,11 +172,6 @@ __device__ __forceinline__ Listed find_listed(const AttnArgs& p, int64_t item, c
         if (n > 0) {
             r.b = b0 + n - 1;
             r.q = lane_seq(p, g, n - 1);
-        }
-        if (WEIGHTS) {
-            const int64_t w = group_seq(p, g).weight, upto = wave_scan(w);
-            if (n > 0) r.before = (done + lane_value(upto - w, n - 1)) * p.a.heads;
-            done += lane_value(upto, kWave - 1);
         }
         b0 += kWave;
         if (n < kWave || b0 >= p.a.B) return r;
@@ -193,14 +186,14 @@ __device__ __forceinline__ int xcd_worker(int L, int W) {
     return x * base + (x < rem ? x : rem) + L / kXcds;
 }
 
-// The tile at a worker's position and what it does of it; moves the position on.  False
-// at the end of the worker's part.
+// The tile at a worker's position and what it does of it; moves the position on, and
+// leaves the record of a tile that goes on in a later worker's part.  False at the end.
 struct Tile {
     Seq s;
     int b, h, r;
     AttnPart part;
 };
-__device__ __forceinline__ bool next_tile(const AttnArgs& p, Share& sh, Tile& t) {
+__device__ __forceinline__ bool next_tile(const AttnArgs& p, Share& sh, int worker, Tile& t) {
     while (sh.at < sh.end && sh.b < p.a.B) {
         const AttnSeq q = scalar_seq(p, sh.b);
         const int64_t weight = q.weight * p.a.heads;
@@ -213,7 +206,12 @@ __device__ __forceinline__ bool next_tile(const AttnArgs& p, Share& sh, Tile& t)
         const int r = attn_find_tile(q, sh.at - sh.before - h * q.weight);
         t = {q.s, sh.b, h, r, attn_part(p.a, q, sh.before, h, r, sh.at, sh.end)};
         sh.at = t.part.next;
-        if (t.part.k0 < t.part.k1 || t.part.whole) return true;
+        if (t.part.ends_inside && !t.part.begins_inside) {
+            const int64_t past = sh.before + h * q.weight + attn_before(q, r) + q.base + q.slope * r;
+            if (threadIdx.x % kWave == 0)
+                p.records[worker] = {attn_worker(sh.cut, past - 1), q.s.t0, q.s.n * p.a.G, r * p.a.rows, h, {0, 0, 0}};
+        }
+        return true;
     }
     return false;
 }

@@ -117,27 +117,42 @@ SQ_HD int attn_cut(int64_t x, int64_t weight, int count) {
 // What a worker that stands at position `at` and ends at `end` does of tile r of key
 // head h: steps [k0, k1), where it stands next, whether these are all of the tile's
 // (a tile without steps is its first worker's, which writes zeros), and whether its
-// part begins inside the tile.
+// part begins and ends inside the tile.
 struct AttnPart {
     int64_t next;
     int k0, k1;
-    bool whole, inside;
+    bool whole, begins_inside, ends_inside;
 };
 SQ_HD AttnPart attn_part(const AttnShape& a, const AttnSeq& q, int64_t before, int h, int r, int64_t at, int64_t end) {
     const int64_t weight = q.base + q.slope * r, from = before + h * q.weight + attn_before(q, r);
     const int64_t x0 = at - from, x1 = end - from < weight ? end - from : weight;
     const AttnSteps s = attn_steps(a, q.s, r);
     const int k0 = attn_cut(x0, weight, s.count), k1 = attn_cut(x1, weight, s.count);
-    return {from + x1, s.first + k0, s.first + k1, k1 - k0 == s.count && (s.count > 0 || x0 == 0), x0 > 0};
+    return {from + x1, s.first + k0, s.first + k1, k1 - k0 == s.count && (s.count > 0 || x0 == 0), x0 > 0, x1 < weight};
 }
 
-// Partial results: two places for each worker, the tile its part begins inside of
-// and the tile it ends inside of.  A place holds, per row, D sums in fp32, the
-// maximum and the sum of the row's softmax.
+// The workspace of a batch whose tiles are shared out.  Every worker has a record and
+// two places for partial results: of the tile its part begins inside of, and of the one
+// that begins in its part and ends in a later worker's.  The record is of the second:
+// the joining kernel finds there what to join, from this worker's place for it and the
+// first places of the workers up to `last`; -1: nothing.  A worker that has no step of
+// a tile, or all of them and wrote the rows, leaves its place without a maximum (-inf).
+struct AttnRecord {
+    int last;             // last worker of the tile, or -1
+    int t0, rows;         // the sequence's first row of the batch, its rows of a key head
+    int row0;             // the tile's first
+    int h;
+    int unused[3];
+};
 SQ_HD int attn_place(int w, bool begins_inside) { return 2 * w + (begins_inside ? 0 : 1); }
+// Per row of a tile: D sums in fp32, the reference and the sum of the row's softmax.
 SQ_HD int64_t attn_place_floats(int rows, int D) { return (int64_t)rows * (D + 2); }
+inline int64_t attn_workspace(const AttnShape& a, int D) {
+    return a.workers * ((int64_t)sizeof(AttnRecord) + 2 * attn_place_floats(a.rows, D) * 4);
+}
 
-// Tiles of all sequences and key heads, at most: what the joining kernel's grid covers.
+// Tiles of all sequences and key heads, at most: places in a list where a batch is read
+// tile by tile.
 inline int64_t attn_tile_slots(const AttnShape& a) { return ((int64_t)a.T * a.G / a.rows + a.B) * a.heads; }
 
 // Whether a batch is read with a workgroup for each tile instead, none split and

@@ -57,26 +57,26 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_tile_kernel(AttnA
     const int G = p.a.G, D = p.D, R = p.a.rows;
     const Group first = load_group(p, 0, lane);
     const Survey all = survey(p, first, lane);
-    Share sh{0, 0, 0, 0};
+    Share sh{};
     Tile tile{};
-    int worker = 0;
+    const int worker = xcd_worker(blockIdx.x, p.a.groups);
+    if (!attn_always_direct(p.a) && (int)blockIdx.x < p.a.groups && tid == 0) p.records[worker].last = -1;
     if (all.direct) {
         const int64_t tiles = gridDim.x / p.a.heads;
         const int64_t at = xcd_worker(blockIdx.x, gridDim.x);
         const int64_t item = at % tiles;               // a head's tiles run on one XCD
         if (at / tiles >= p.a.heads) return;
-        const Listed l = find_listed<false>(p, item, first, lane);
+        const Listed l = find_listed(p, item, first, lane);
         const int64_t r64 = item - list_start(l.q.s.t0, l.b, G, R, 1);
         if (r64 < 0 || r64 >= l.q.tiles) return;
         const AttnSteps steps = attn_steps(p.a, l.q.s, (int)r64);
-        tile = {l.q.s, l.b, (int)(at / tiles), (int)r64, {0, steps.first, steps.first + steps.count, true, false}};
+        tile = {l.q.s, l.b, (int)(at / tiles), (int)r64, {0, steps.first, steps.first + steps.count, true, false, false}};
     } else {
         if ((int)blockIdx.x >= p.a.groups) return;
-        worker = xcd_worker(blockIdx.x, p.a.groups);
         sh = find_share(p, all.total, first, worker, lane);
     }
     for (;;) {
-        if (!all.direct && !next_tile(p, sh, tile)) return;
+        if (!all.direct && !next_tile(p, sh, worker, tile)) return;
         const Seq seq{__builtin_amdgcn_readfirstlane(tile.s.t0), __builtin_amdgcn_readfirstlane(tile.s.n),
                       __builtin_amdgcn_readfirstlane(tile.s.len), __builtin_amdgcn_readfirstlane(tile.s.off)};
         const AttnPart& part = tile.part;
@@ -314,7 +314,8 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_tile_kernel(AttnA
             const int64_t o = (int64_t)t * p.a.heads * G + qh;
             const int lr = wave * 32 + c;
             const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-            float* ws = part.whole ? nullptr : p.ws + attn_place(worker, part.inside) * attn_place_floats(R, D);
+            const bool split = part.begins_inside || part.ends_inside, any = s0 < s1 && !part.whole;
+            float* ws = p.places + attn_place(worker, part.begins_inside) * attn_place_floats(R, D);
 #pragma unroll
             for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -323,12 +324,12 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_tile_kernel(AttnA
                     const f4 x{O[d][4 * e], O[d][4 * e + 1], O[d][4 * e + 2], O[d][4 * e + 3]};
                     if (ch < D) {
                         if (part.whole) store_result(p.O + o * D + ch, x, inv);
-                        else *reinterpret_cast<f4*>(ws + lr * D + ch) = x;
+                        else if (any) *reinterpret_cast<f4*>(ws + lr * D + ch) = x;
                     }
                 }
             if (half == 0) {
-                if (!part.whole) ws[R * D + lr] = m, ws[R * D + R + lr] = l;
-                else if (p.lse) p.lse[o] = result_lse(m, l);
+                if (split) ws[R * D + lr] = any ? m : kNone, ws[R * D + R + lr] = l;
+                if (part.whole && p.lse) p.lse[o] = result_lse(m, l);
             }
         }
         if (all.direct) return;

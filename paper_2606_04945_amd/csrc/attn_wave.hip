@@ -202,16 +202,19 @@ struct WaveRows {
         }
     }
 
-    __device__ __forceinline__ void store_partial(const AttnArgs& p, float* ws, int c, int g) const {
+    // `any` false: this worker's place of the tile holds nothing to join
+    __device__ __forceinline__ void store_partial(const AttnArgs& p, float* ws, bool any, int c, int g) const {
         constexpr int R = 16 * QT;
 #pragma unroll
         for (int y = 0; y < QT; ++y) {
             if (!in[y]) continue;
             const int row = 16 * y + c;
+            if (any) {
 #pragma unroll
-            for (int d = 0; d < DT; ++d)
-                if (16 * d < p.D) *reinterpret_cast<f4*>(ws + row * p.D + 16 * d + 4 * g) = O[y][d];
-            if (g == 0) ws[R * p.D + row] = m[y], ws[R * p.D + R + row] = l[y];
+                for (int d = 0; d < DT; ++d)
+                    if (16 * d < p.D) *reinterpret_cast<f4*>(ws + row * p.D + 16 * d + 4 * g) = O[y][d];
+            }
+            if (g == 0) ws[R * p.D + row] = any ? m[y] : kNone, ws[R * p.D + R + row] = l[y];
         }
     }
 };
@@ -227,34 +230,35 @@ __global__ __launch_bounds__(NW* kWave) void attn_wave_kernel(AttnArgs p) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const Group first = load_group(p, 0, lane);
     const Survey all = survey(p, first, lane);
-    Share sh{0, 0, 0, 0};
+    Share sh{};
     Tile t{};
-    int worker = 0, stride = 1, count = 0;
+    int stride = 1, count = 0;
+    const int worker = xcd_worker(blockIdx.x, p.a.groups) * NW + wave;
+    if (!attn_always_direct(p.a) && (int)blockIdx.x < p.a.groups && lane == 0) p.records[worker].last = -1;
     if (all.direct) {
         const int64_t item = blockIdx.x / p.a.heads;
-        const Listed at = find_listed<false>(p, item, first, lane);
+        const Listed at = find_listed(p, item, first, lane);
         const int64_t r64 = item - list_start(at.q.s.t0, at.b, p.a.G, R, 1);
         if (r64 < 0 || r64 >= at.q.tiles) return;
         const AttnSteps steps = attn_steps(p.a, at.q.s, (int)r64);
         count = steps.count;
         stride = NW;
         t = {at.q.s, at.b, (int)(blockIdx.x % p.a.heads), (int)r64,
-             {0, steps.first + wave, steps.first + steps.count, false, false}};
+             {0, steps.first + wave, steps.first + steps.count, false, false, false}};
     } else {
         if ((int)blockIdx.x >= p.a.groups) return;
-        worker = xcd_worker(blockIdx.x, p.a.groups) * NW + wave;
         sh = find_share(p, all.total, first, worker, lane);
     }
     for (;;) {
-        if (!all.direct && !next_tile(p, sh, t)) return;
+        if (!all.direct && !next_tile(p, sh, worker, t)) return;
         WaveRows<DP, QT> w;
         w.begin(p, t.s, t.h, t.r, c, g);
         w.pass(p, t.s, t.b, t.h, t.part.k0, t.part.k1, stride, c, g);
         if (!all.direct) {
-            if (t.part.whole)
-                w.store(p, g);
-            else
-                w.store_partial(p, p.ws + attn_place(worker, t.part.inside) * attn_place_floats(R, p.D), c, g);
+            if (t.part.whole) w.store(p, g);
+            if (t.part.begins_inside || t.part.ends_inside)
+                w.store_partial(p, p.places + attn_place(worker, t.part.begins_inside) * attn_place_floats(R, p.D),
+                                t.part.k0 < t.part.k1 && !t.part.whole, c, g);
             continue;
         }
         const int waves = min(count, NW);              // those that had a step

@@ -35,52 +35,69 @@ extern "C" int walk(int T, int B, int heads, int G, int max_len, int causal, int
     }
     typedef std::tuple<int, int, int> Tile;
     std::map<Tile, std::vector<int>> read;                 // how often each step is read
-    std::map<Tile, std::set<int>> written;                 // places of partial results
+    std::map<Tile, std::map<int, bool>> written;           // places: whether they hold a result
     std::map<Tile, int> direct;
     std::set<int> places;
+    std::vector<AttnRecord> records(a.workers);
+    std::vector<Tile> recorded(a.workers);
     int64_t most = 0, least = INT64_MAX;
     const AttnCut cut = attn_cut_work(total, a.workers);
     if (attn_start(cut, 0) != 0 || attn_start(cut, a.workers) != total) return 16;
     for (int w = 0; w < a.workers; ++w) {
+        records[w].last = -1;
         int64_t at = attn_start(cut, w), end = attn_start(cut, w + 1), did = 0;
         if (end < at) return 4;
-        if (at >= end) continue;
         int b = 0;
-        while (before[b] + s[b].weight * heads <= at) ++b;
         while (at < end) {
             if (b >= B) return 5;
             const AttnSeq& q = s[b];
-            if (q.weight == 0) { ++b; continue; }
-            const int h = (int)((at - before[b]) / q.weight);
+            if (at - before[b] >= q.weight * heads) { ++b; continue; }
+            const int h = (int)divide(at - before[b], q.weight);
             if (h < 0 || h >= heads) return 6;
-            int r = attn_find_tile(q, at - before[b] - h * q.weight);
-            for (; r < q.tiles && at < end; ++r) {
-                const int64_t weight = q.base + q.slope * r, from = before[b] + h * q.weight + attn_before(q, r);
-                if (at < from || at >= from + weight) return 7;
-                const AttnPart part = attn_part(a, q, before[b], h, r, at, end);
-                if (part.next <= at || part.next > end || part.next > from + weight) return 7;
-                at = part.next;
-                const AttnSteps st = attn_steps(a, q.s, r);
-                if (st.count < 0 || st.first < 0 || (st.count && (int64_t)(st.first + st.count - 1) * kAttnStep >= q.s.len)) return 8;
-                if (part.k0 == part.k1 && !part.whole) continue;
-                Tile t(b, h, r);
-                read[t].resize(st.count);
-                if (part.k0 < st.first || part.k1 > st.first + st.count || part.k1 < part.k0) return 17;
-                for (int k = part.k0; k < part.k1; ++k) ++read[t][k - st.first];
-                did += part.k1 - part.k0;
-                if (part.whole) ++direct[t];
-                else {
-                    const int place = attn_place(w, part.inside);
-                    if (place < 0 || place >= 2 * a.workers || !places.insert(place).second) return 9;
-                    written[t].insert(place);
-                }
+            const int r = attn_find_tile(q, at - before[b] - h * q.weight);
+            const int64_t weight = q.base + q.slope * r, from = before[b] + h * q.weight + attn_before(q, r);
+            if (at < from || at >= from + weight) return 7;
+            const AttnPart part = attn_part(a, q, before[b], h, r, at, end);
+            if (part.next <= at || part.next > end || part.next > from + weight) return 7;
+            if (part.begins_inside != (at > from) || part.ends_inside != (part.next < from + weight)) return 18;
+            const Tile t(b, h, r);
+            if (part.ends_inside && !part.begins_inside) {
+                if (records[w].last >= 0) return 19;
+                records[w] = {attn_worker(cut, from + weight - 1), q.s.t0, q.s.n * G, r * rows, h, {0, 0, 0}};
+                recorded[w] = t;
+                if (records[w].last <= w || records[w].last >= a.workers) return 20;
             }
-            if (r == q.tiles && at - before[b] >= q.weight * heads) ++b;
+            at = part.next;
+            const AttnSteps st = attn_steps(a, q.s, r);
+            if (st.count < 0 || st.first < 0 || (st.count && (int64_t)(st.first + st.count - 1) * kAttnStep >= q.s.len)) return 8;
+            if (part.k0 < st.first || part.k1 > st.first + st.count || part.k1 < part.k0) return 17;
+            read[t].resize(st.count);
+            for (int k = part.k0; k < part.k1; ++k) ++read[t][k - st.first];
+            did += part.k1 - part.k0;
+            direct[t] += part.whole;
+            if (part.begins_inside || part.ends_inside) {
+                const int place = attn_place(w, part.begins_inside);
+                if (place < 0 || place >= 2 * a.workers || !places.insert(place).second) return 9;
+                written[t][place] = part.k0 < part.k1 && !part.whole;
+            } else if (!part.whole) return 21;
         }
+        if (attn_start(cut, w) >= end) continue;
         most = std::max(most, did);
         least = std::min(least, did);
     }
     int64_t slots = attn_tile_slots(a);
+    std::map<Tile, int> joined;
+    for (int w = 0; w < a.workers; ++w)
+        if (records[w].last >= 0) {
+            std::map<int, bool> join;
+            for (int j = w; j <= records[w].last; ++j) {
+                const int place = attn_place(j, j > w);
+                if (!written[recorded[w]].count(place)) return 22;
+                join[place] = written[recorded[w]][place];
+            }
+            if (join != written[recorded[w]]) return 23;
+            ++joined[recorded[w]];
+        }
     long long split = 0;
     for (int b = 0; b < B; ++b) {
         const AttnSeq& q = s[b];
@@ -96,24 +113,17 @@ extern "C" int walk(int T, int B, int heads, int G, int max_len, int causal, int
                     const int p = q.s.off + (int)(row / G), lo = attn_lo(a, p), hi = attn_hi(a, q.s, p);
                     if (hi > lo && (lo < st.first * kAttnStep || hi > (st.first + st.count) * kAttnStep)) return 12;
                 }
-                // what the joining workgroup finds
+                // a batch read tile by tile finds every tile
                 const int64_t item = list_start(q.s.t0, b, G, rows, 1) + r;
                 if (item * heads + h >= slots) return 13;
                 int lo = -1;
                 for (int i = 0; i < B; ++i) lo += list_start(std::min(std::max(cu[i], 0), T), i, G, rows, 1) <= item;
                 if (lo != b) return 14;
-                const int64_t from = before[b] + h * q.weight + attn_before(q, r), weight = q.base + q.slope * r;
-                const int w0 = attn_worker(cut, from), w1 = attn_worker(cut, from + weight - 1);
-                std::set<int> join;
-                bool alone = st.count <= 1 || w0 == w1;
-                for (int w = w0; w <= w1 && !alone; ++w) {
-                    const int64_t x0 = attn_start(cut, w) - from, x1 = std::min(attn_start(cut, w + 1) - from, weight);
-                    const int k0 = attn_cut(x0, weight, st.count), k1 = attn_cut(x1, weight, st.count);
-                    alone = k1 - k0 == st.count;
-                    if (k1 > k0) join.insert(attn_place(w, x0 > 0));
-                }
-                if (alone ? direct[t] != 1 || !written[t].empty() : direct[t] != 0 || join != written[t]) return 15;
-                split += !alone;
+                // written by one worker, or joined from results, once
+                bool any = false;
+                for (auto& x : written[t]) any |= x.second;
+                if (direct[t] != !any || joined[t] != !written[t].empty()) return 15;
+                split += any;
             }
     }
     stats[0] = most; stats[1] = least; stats[2] = split; stats[3] = a.workers;
