@@ -45,11 +45,20 @@ namespace {
 
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef float f2 __attribute__((ext_vector_type(2)));
 typedef float f4 __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kNone = -__builtin_inff();
+
+// Stores through pointers that are known to be global.  From a pointer of no known
+// space the compiler makes a flat store, and while one may be pending every wait for a
+// load is a wait for all loads: the loops over keys would have none in flight.
+template <class T>
+__device__ __forceinline__ void store_global(void* p, const T& x) {
+    *(__attribute__((address_space(1))) T*)p = x;
+}
 
 // Sum over the lanes up to this one: shifts within rows of 16 lanes, then the rows'
 // last lanes spread to the rows after them.
@@ -208,8 +217,11 @@ __device__ __forceinline__ bool next_tile(const AttnArgs& p, Share& sh, int work
         sh.at = t.part.next;
         if (t.part.ends_inside && !t.part.begins_inside) {
             const int64_t past = sh.before + h * q.weight + attn_before(q, r) + q.base + q.slope * r;
-            if (threadIdx.x % kWave == 0)
-                p.records[worker] = {attn_worker(sh.cut, past - 1), q.s.t0, q.s.n * p.a.G, r * p.a.rows, h, {0, 0, 0}};
+            if (threadIdx.x % kWave == 0) {
+                AttnRecord* record = p.records + worker;
+                store_global(record, v4i{attn_worker(sh.cut, past - 1), q.s.t0, q.s.n * p.a.G, r * p.a.rows});
+                store_global(&record->h, h);
+            }
         }
         return true;
     }
@@ -262,10 +274,9 @@ __device__ __forceinline__ h8 load_query(const uint16_t* q, uint32_t flip) {
 
 // four results of a row as fp16
 __device__ __forceinline__ void store_result(uint16_t* o, f4 x, float inv) {
-    uint2 w;
-    w.x = (uint32_t)f2h(x[0] * inv) | ((uint32_t)f2h(x[1] * inv) << 16);
-    w.y = (uint32_t)f2h(x[2] * inv) | ((uint32_t)f2h(x[3] * inv) << 16);
-    *reinterpret_cast<uint2*>(o) = w;
+    const u32x2 w = {(uint32_t)f2h(x[0] * inv) | ((uint32_t)f2h(x[1] * inv) << 16),
+                     (uint32_t)f2h(x[2] * inv) | ((uint32_t)f2h(x[3] * inv) << 16)};
+    store_global(o, w);
 }
 
 __device__ __forceinline__ float result_lse(float m, float l) {

@@ -60,7 +60,8 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_tile_kernel(AttnA
     Share sh{};
     Tile tile{};
     const int worker = xcd_worker(blockIdx.x, p.a.groups);
-    if (!attn_always_direct(p.a) && (int)blockIdx.x < p.a.groups && tid == 0) p.records[worker].last = -1;
+    if (!attn_always_direct(p.a) && (int)blockIdx.x < p.a.groups && tid == 0)
+        store_global(&p.records[worker].last, -1);
     if (all.direct) {
         const int64_t tiles = gridDim.x / p.a.heads;
         const int64_t at = xcd_worker(blockIdx.x, gridDim.x);
@@ -324,12 +325,15 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_tile_kernel(AttnA
                     const f4 x{O[d][4 * e], O[d][4 * e + 1], O[d][4 * e + 2], O[d][4 * e + 3]};
                     if (ch < D) {
                         if (part.whole) store_result(p.O + o * D + ch, x, inv);
-                        else if (any) *reinterpret_cast<f4*>(ws + lr * D + ch) = x;
+                        else if (any) store_global(ws + lr * D + ch, x);
                     }
                 }
             if (half == 0) {
-                if (split) ws[R * D + lr] = any ? m : kNone, ws[R * D + R + lr] = l;
-                if (part.whole && p.lse) p.lse[o] = result_lse(m, l);
+                if (split) {
+                    store_global(ws + R * D + lr, any ? m : kNone);
+                    store_global(ws + R * D + R + lr, l);
+                }
+                if (part.whole && p.lse) store_global(p.lse + o, result_lse(m, l));
             }
         }
         if (all.direct) return;

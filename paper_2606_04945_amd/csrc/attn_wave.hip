@@ -21,9 +21,19 @@ __device__ __forceinline__ float groups_sum(float x) {
     return x + __shfl_xor(x, 32, kWave);
 }
 
+// A load that the scheduler leaves in its place.  What enters a loop and what comes
+// round it then have the same loads in flight in the same order, and the wait for one
+// of them need not be a wait for all.
+template <class T>
+__device__ __forceinline__ T load_in_order(const void* p) {
+    const T x = *static_cast<const T*>(p);
+    __builtin_amdgcn_sched_barrier(0);
+    return x;
+}
+
 // One wave's rows of a tile: 16 QT of them, and the pass over some of their steps.
-// DP: head size rounded up to 64, 128 or 256.
-template <int DP, int QT>
+// DP: head size rounded up to 64, 128 or 256.  WIDE: pages of 64 tokens and more.
+template <int DP, int QT, bool WIDE>
 struct WaveRows {
     static constexpr int P = DP / 64, DT = DP / 16;
     int t[QT], qh[QT], lo[QT], hi[QT];    // batch row, query head, visible keys of this lane's column
@@ -55,72 +65,96 @@ struct WaveRows {
         }
     }
 
-    // What a step reads, a lane's part: the pages of its key row (group c / 4 of the step)
-    // and of its lane group's keys, codes and scales.  Every load is issued on every step
-    // (addresses are kept inside instead), so that waiting for some leaves the others in
-    // flight.
+    // What a step reads, a lane's part.  Every load is issued on every step (addresses are
+    // kept inside instead), so that waiting for some leaves the others in flight.
     struct Reads {
-        int kp, vp;                               // pages, -1: none
+        bool in;                                  // this lane group's keys have a page
         v4i k[4][P], v[DT];
         float ks, vs;
     };
-    __device__ __forceinline__ void pages(const AttnArgs& p, const Seq& s, const int32_t* table, int kt, int c, int g,
-                                          int& kp, int& vp) const {
-        const int ka = kt * kAttnStep + 16 * (c / 4), va = kt * kAttnStep + 16 * g;
-        const int k = table[min(ka, s.len - 1) >> p.shift], v = table[min(va, s.len - 1) >> p.shift];
-        kp = ka < s.len && (uint32_t)k < (uint32_t)p.pages ? k : -1;
-        vp = va < s.len && (uint32_t)v < (uint32_t)p.pages ? v : -1;
+
+    // The pass over steps first, first + stride, ... below end.  64 page table entries are
+    // held, one a lane, in the order in which the steps need them.
+    struct Pages {
+        const int32_t* table;
+        int held, first, stride;                  // entries of the sequence; the steps
+        int per, ids;                             // entries a step; this lane's page, -1: none
+    };
+    __device__ __forceinline__ void hold(const AttnArgs& p, Pages& q, int j, int lane) const {
+        const int at = ((q.first + (j + lane / q.per) * q.stride) * kAttnStep >> p.shift) + lane % q.per;
+        const int id = q.table[min(at, q.held - 1)];
+        q.ids = at < q.held && (uint32_t)id < (uint32_t)p.pages ? id : -1;
     }
-    __device__ __forceinline__ void keys(const AttnArgs& p, int h, int kt, int c, int g, Reads& r) const {
-        const int ka = kt * kAttnStep + 16 * (c / 4);
-        const int64_t ph = r.kp >= 0 ? (int64_t)r.kp * p.a.heads + h : h;
-        const int8_t* at = p.k + (ph * p.page + (ka & (p.page - 1)) + c % 4) * p.D;
+    __device__ __forceinline__ int64_t head_of(const AttnArgs& p, int pid, int h) const {
+        return pid >= 0 ? (int64_t)pid * p.a.heads + h : (int64_t)h;
+    }
+    // Keys and scales, and values, of the pass's step j.  WIDE: one page a step, addresses
+    // from scalar registers; otherwise a lane has the page of its key row (group c / 4 of the
+    // step) and that of its lane group.  Past the channels the keys are others again, which
+    // meet zero queries, and the values too, which are not stored.
+    __device__ __forceinline__ void keys(const AttnArgs& p, const Pages& q, int h, int j, int c, int g, Reads& r) const {
+        const int key0 = (q.first + j * q.stride) * kAttnStep, entry = j * q.per & (kWave - 1);
+        int64_t ph;
+        const int8_t* at;
+        if (WIDE) {
+            const int pid = __builtin_amdgcn_readlane(q.ids, entry);
+            r.in = pid >= 0;
+            ph = head_of(p, pid, h);
+            at = p.k + (ph * p.page + (key0 & (p.page - 1))) * p.D;
+        } else {
+            const int kp = __shfl(q.ids, entry + (16 * (c / 4) >> p.shift), kWave);
+            const int vp = __shfl(q.ids, entry + (16 * g >> p.shift), kWave);
+            r.in = vp >= 0;
+            ph = head_of(p, vp, h);
+            at = p.k + (head_of(p, kp, h) * p.page + (16 * (c / 4) & (p.page - 1)) - 16 * (c / 4)) * p.D;
+        }
+        const int row = (16 * (c / 4) + c % 4) * p.D;
 #pragma unroll
         for (int e = 0; e < 4; ++e)
 #pragma unroll
-            for (int z = 0; z < P; ++z)           // past the channels: others again, which meet zero queries
-                r.k[e][z] = *reinterpret_cast<const v4i*>(at + 4 * e * p.D + min(64 * z + 16 * g, p.D - 16));
+            for (int z = 0; z < P; ++z)
+                r.k[e][z] = load_in_order<v4i>(at + 4 * e * p.D + (uint32_t)(row + min(64 * z + 16 * g, p.D - 16)));
+        r.ks = load_in_order<float>(p.k_scale + ph);
+        r.vs = load_in_order<float>(p.v_scale + ph);
     }
-    __device__ __forceinline__ void values(const AttnArgs& p, int h, int kt, int c, int g, Reads& r) const {
-        const int64_t ph = r.vp >= 0 ? (int64_t)r.vp * p.a.heads + h : h;
-        const int8_t* at = p.v + ph * p.page * p.D + ((kt * kAttnStep + 16 * g) & (p.page - 1));
+    __device__ __forceinline__ void values(const AttnArgs& p, const Pages& q, int h, int j, int c, int g, Reads& r) const {
+        const int key0 = (q.first + j * q.stride) * kAttnStep, entry = j * q.per & (kWave - 1);
+        const int8_t* at;
+        if (WIDE) {
+            at = p.v + head_of(p, __builtin_amdgcn_readlane(q.ids, entry), h) * p.page * p.D + (key0 & (p.page - 1));
+        } else {
+            const int vp = __shfl(q.ids, entry + (16 * g >> p.shift), kWave);
+            at = p.v + head_of(p, vp, h) * p.page * p.D + (16 * g & (p.page - 1)) - 16 * g;
+        }
 #pragma unroll
         for (int d = 0; d < DT; ++d)
-            r.v[d] = *reinterpret_cast<const v4i*>(at + min(16 * d + c, p.D - 1) * p.page);
-    }
-    __device__ __forceinline__ void scales(const AttnArgs& p, int h, Reads& r) const {
-        const int64_t ph = r.vp >= 0 ? (int64_t)r.vp * p.a.heads + h : h;
-        r.ks = p.k_scale[ph];
-        r.vs = p.v_scale[ph];
+            r.v[d] = load_in_order<v4i>(at + min(16 * d, p.D - 16) * p.page + (uint32_t)(c * p.page + 16 * g));
     }
 
-    // Steps first, first + stride, ... below end.  What the next step reads is requested as
-    // soon as the registers of this one's are free: its keys before this step's softmax,
-    // its values after the second product, its pages a step earlier.
+    // What the next step reads is requested as soon as the registers of this one's are
+    // free: its keys before this step's softmax, its values after the second product.
     __device__ __forceinline__ void pass(const AttnArgs& p, const Seq& s, int b, int h, int first, int end, int stride,
-                                         int c, int g) {
+                                         int lane) {
+        const int c = lane % 16, g = lane / 16;
         if (first < end) {
-            const int32_t* table = p.table + (int64_t)b * p.max_pages;
+            const int n = (end - first + stride - 1) / stride, per = WIDE ? 1 : kAttnStep >> p.shift;
+            Pages q{p.table + (int64_t)b * p.max_pages, (s.len + p.page - 1) >> p.shift, first, stride, per, -1};
             Reads r;
-            pages(p, s, table, first, c, g, r.kp, r.vp);
-            int kn, vn;                           // pages of the next step
-            pages(p, s, table, first + stride, c, g, kn, vn);
-            keys(p, h, first, c, g, r);
-            scales(p, h, r);
-            values(p, h, first, c, g, r);
-            int kt = first;
-            for (; kt + stride < end; kt += stride) step<true>(p, s, table, h, kt, stride, c, g, r, kn, vn);
-            step<false>(p, s, table, h, kt, stride, c, g, r, kn, vn);
+            hold(p, q, 0, lane);
+            keys(p, q, h, 0, c, g, r);
+            values(p, q, h, 0, c, g, r);
+            for (int j = 0; j + 1 < n; ++j) step<true>(p, q, h, j, lane, r);
+            step<false>(p, q, h, n - 1, lane, r);
         }
 #pragma unroll
         for (int y = 0; y < QT; ++y) l[y] = groups_sum(l[y]);
     }
 
     template <bool MORE>
-    __device__ __forceinline__ void step(const AttnArgs& p, const Seq& s, const int32_t* table, int h, int kt, int stride,
-                                         int c, int g, Reads& r, int& kn, int& vn) {
-        const int key0 = kt * kAttnStep, va = key0 + 16 * g;
-        const BlockScale bs = block_scale(r.vp >= 0, r.ks, r.vs, p.scale);
+    __device__ __forceinline__ void step(const AttnArgs& p, Pages& q, int h, int j, int lane, Reads& r) {
+        const int c = lane % 16, g = lane / 16;
+        const int key0 = (q.first + j * q.stride) * kAttnStep, va = key0 + 16 * g;
+        const BlockScale bs = block_scale(r.in, r.ks, r.vs, p.scale);
         f4 S[QT][4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -135,10 +169,8 @@ struct WaveRows {
             }
         }
         if (MORE) {
-            r.kp = kn, r.vp = vn;
-            keys(p, h, kt + stride, c, g, r);
-            scales(p, h, r);
-            pages(p, s, table, kt + 2 * stride, c, g, kn, vn);
+            if (((j + 1) * q.per & (kWave - 1)) == 0) hold(p, q, j + 1, lane);
+            keys(p, q, h, j + 1, c, g, r);
         }
         h8 W[QT][2];
 #pragma unroll
@@ -186,7 +218,7 @@ struct WaveRows {
                 for (int y = 0; y < QT; ++y)
                     O[y][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, W[y][u], O[y][d], 0, 0, 0);
             }
-        if (MORE) values(p, h, kt + stride, c, g, r);
+        if (MORE) values(p, q, h, j + 1, c, g, r);
     }
 
     __device__ __forceinline__ void store(const AttnArgs& p, int g) const {
@@ -198,7 +230,7 @@ struct WaveRows {
 #pragma unroll
             for (int d = 0; d < DT; ++d)
                 if (16 * d < p.D) store_result(p.O + o * p.D + 16 * d + 4 * g, O[y][d], inv);
-            if (p.lse && g == 0) p.lse[o] = result_lse(m[y], l[y]);
+            if (p.lse && g == 0) store_global(p.lse + o, result_lse(m[y], l[y]));
         }
     }
 
@@ -212,16 +244,19 @@ struct WaveRows {
             if (any) {
 #pragma unroll
                 for (int d = 0; d < DT; ++d)
-                    if (16 * d < p.D) *reinterpret_cast<f4*>(ws + row * p.D + 16 * d + 4 * g) = O[y][d];
+                    if (16 * d < p.D) store_global(ws + row * p.D + 16 * d + 4 * g, O[y][d]);
             }
-            if (g == 0) ws[R * p.D + row] = any ? m[y] : kNone, ws[R * p.D + R + row] = l[y];
+            if (g == 0) {
+                store_global(ws + R * p.D + row, any ? m[y] : kNone);
+                store_global(ws + R * p.D + R + row, l[y]);
+            }
         }
     }
 };
 
 // Direct: a workgroup is a tile, whose steps go round its waves, and their results
 // meet in LDS.  Otherwise every wave is a worker of the shared work.
-template <int DP, int QT, int NW>
+template <int DP, int QT, int NW, bool WIDE>
 __global__ __launch_bounds__(NW* kWave) void attn_wave_kernel(AttnArgs p) {
     extern __shared__ __attribute__((aligned(16))) float lds[];
     constexpr int R = 16 * QT, LD = DP + 4;            // rows, padded row of floats
@@ -234,7 +269,8 @@ __global__ __launch_bounds__(NW* kWave) void attn_wave_kernel(AttnArgs p) {
     Tile t{};
     int stride = 1, count = 0;
     const int worker = xcd_worker(blockIdx.x, p.a.groups) * NW + wave;
-    if (!attn_always_direct(p.a) && (int)blockIdx.x < p.a.groups && lane == 0) p.records[worker].last = -1;
+    if (!attn_always_direct(p.a) && (int)blockIdx.x < p.a.groups && lane == 0)
+        store_global(&p.records[worker].last, -1);
     if (all.direct) {
         const int64_t item = blockIdx.x / p.a.heads;
         const Listed at = find_listed(p, item, first, lane);
@@ -251,9 +287,9 @@ __global__ __launch_bounds__(NW* kWave) void attn_wave_kernel(AttnArgs p) {
     }
     for (;;) {
         if (!all.direct && !next_tile(p, sh, worker, t)) return;
-        WaveRows<DP, QT> w;
+        WaveRows<DP, QT, WIDE> w;
         w.begin(p, t.s, t.h, t.r, c, g);
-        w.pass(p, t.s, t.b, t.h, t.part.k0, t.part.k1, stride, c, g);
+        w.pass(p, t.s, t.b, t.h, t.part.k0, t.part.k1, stride, lane);
         if (!all.direct) {
             if (t.part.whole) w.store(p, g);
             if (t.part.begins_inside || t.part.ends_inside)
@@ -292,22 +328,28 @@ __global__ __launch_bounds__(NW* kWave) void attn_wave_kernel(AttnArgs p) {
             const int at = t.r * R + row;
             const int64_t o = (int64_t)(t.s.t0 + at / p.a.G) * p.a.heads * p.a.G + t.h * p.a.G + at % p.a.G;
             store_result(p.O + o * p.D + d, O, l > 0.0f ? 1.0f / l : 0.0f);
-            if (p.lse && d == 0) p.lse[o] = result_lse(m, l);
+            if (p.lse && d == 0) store_global(p.lse + o, result_lse(m, l));
         }
         return;
     }
 }
 
-template <int DP, int QT>
-hipError_t launch(const AttnArgs& p, hipStream_t st) {
+template <int DP, int QT, bool WIDE>
+hipError_t launch_pages(const AttnArgs& p, hipStream_t st) {
     constexpr int NW = DP * QT <= 128 ? 8 : 4;
     constexpr int bytes = NW * 16 * QT * (DP + 4 + 2) * (int)sizeof(float);
     static std::atomic<int> set[kMaxDevices];
     if (p.a.workers != p.a.groups * NW) return hipErrorInvalidConfiguration;
-    const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(&attn_wave_kernel<DP, QT, NW>), bytes, set);
+    const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(&attn_wave_kernel<DP, QT, NW, WIDE>), bytes, set);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((attn_wave_kernel<DP, QT, NW>), dim3((unsigned)attn_grid(p.a)), dim3(NW * kWave), bytes, st, p);
+    hipLaunchKernelGGL((attn_wave_kernel<DP, QT, NW, WIDE>), dim3((unsigned)attn_grid(p.a)), dim3(NW * kWave), bytes, st,
+                       p);
     return hipGetLastError();
+}
+
+template <int DP, int QT>
+hipError_t launch(const AttnArgs& p, hipStream_t st) {
+    return p.page >= kAttnStep ? launch_pages<DP, QT, true>(p, st) : launch_pages<DP, QT, false>(p, st);
 }
 
 }  // namespace
