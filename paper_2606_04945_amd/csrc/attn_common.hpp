@@ -202,9 +202,10 @@ struct Tile {
     int b, h, r;
     AttnPart part;
 };
-__device__ __forceinline__ bool next_tile(const AttnArgs& p, Share& sh, int worker, Tile& t) {
+template <bool LANES>      // sequences from the lanes that hold them, no load, for three registers
+__device__ __forceinline__ bool next_tile(const AttnArgs& p, const Group& first, Share& sh, int worker, Tile& t) {
     while (sh.at < sh.end && sh.b < p.a.B) {
-        const AttnSeq q = scalar_seq(p, sh.b);
+        const AttnSeq q = LANES && sh.b < kWave ? lane_seq(p, first, sh.b) : scalar_seq(p, sh.b);
         const int64_t weight = q.weight * p.a.heads;
         if (sh.at - sh.before >= weight) {             // also a sequence without rows
             sh.before += weight;

@@ -77,7 +77,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_tile_kernel(AttnA
         sh = find_share(p, all.total, first, worker, lane);
     }
     for (;;) {
-        if (!all.direct && !next_tile(p, sh, worker, tile)) return;
+        if (!all.direct && !next_tile<false>(p, first, sh, worker, tile)) return;
         const Seq seq{__builtin_amdgcn_readfirstlane(tile.s.t0), __builtin_amdgcn_readfirstlane(tile.s.n),
                       __builtin_amdgcn_readfirstlane(tile.s.len), __builtin_amdgcn_readfirstlane(tile.s.off)};
         const AttnPart& part = tile.part;

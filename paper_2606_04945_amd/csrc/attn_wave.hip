@@ -286,7 +286,7 @@ __global__ __launch_bounds__(NW* kWave) void attn_wave_kernel(AttnArgs p) {
         sh = find_share(p, all.total, first, worker, lane);
     }
     for (;;) {
-        if (!all.direct && !next_tile(p, sh, worker, t)) return;
+        if (!all.direct && !next_tile<true>(p, first, sh, worker, t)) return;
         WaveRows<DP, QT, WIDE> w;
         w.begin(p, t.s, t.h, t.r, c, g);
         w.pass(p, t.s, t.b, t.h, t.part.k0, t.part.k1, stride, lane);
