@@ -20,8 +20,11 @@ class KVCacheStruct(ctypes.Structure):
     _fields_ = [("k", _p), ("v", _p), ("k_scale", _p), ("v_scale", _p),
                 ("pages", _i32), ("page", _i32), ("heads", _i32), ("dim", _i32)]
 
+    @property
+    def _as_parameter_(self):          # given to a call by its address
+        return ctypes.byref(self)
 
-_cache = ctypes.POINTER(KVCacheStruct)
+
 SIGNATURES = {
     "sq_last_error": (ctypes.c_char_p, []),
     "sq_version": (ctypes.c_char_p, []),
@@ -58,11 +61,11 @@ SIGNATURES = {
     "sq_rope_frequencies": (ctypes.c_int, [_i32, _f64, _i32, _f64, _f64, _f64, _f64, _p, _p]),
     "sq_rope_amplitude": (_f64, [_i32, _f64]),
     "sq_rope": (ctypes.c_int, [_p, _i64, _i64, _p, _p, _i32, _i32, _i32, _i32, _i32, _i32, _f32, _p, _i64, _i64, _p]),
-    "kv_append": (ctypes.c_int, [_cache, _p, _i64, _i64, _p, _i64, _i64, _p, _p, _p, _i32, _i32, _i32, _p, _p, _i32,
+    "kv_append": (ctypes.c_int, [_p, _p, _i64, _i64, _p, _i64, _i64, _p, _p, _p, _i32, _i32, _i32, _p, _p, _i32,
                                  _i32, _f32, _p, _i64, _i64, _i32, _p, _i64, _i64, _p]),
-    "kv_read": (ctypes.c_int, [_cache, _p, _i32, _p, _p, _p]),
+    "kv_read": (ctypes.c_int, [_p, _p, _i32, _p, _p, _p]),
     "sq_attn_kv8_workspace_bytes": (_sz, [_i32, _i32, _i32, _i32, _i32, _i32]),
-    "attn_kv8": (ctypes.c_int, [_p, _i64, _i64, _cache, _p, _p, _p, _i32, _i32, _i32, _i32, _i32, _i32, _f32, _p, _p,
+    "attn_kv8": (ctypes.c_int, [_p, _i64, _i64, _p, _p, _p, _p, _i32, _i32, _i32, _i32, _i32, _i32, _f32, _p, _p,
                                 _p, _sz, _p]),
     "sq_quantize_weights_group": (ctypes.c_int, [_p, _i32, _i32, _i32, _p, _p, _p]),
     "w4a16_gemm_frag": (ctypes.c_int, [_p, _p, _p, _i32, _i32, _i32, _i32, _p, _p]),
