@@ -355,7 +355,7 @@ int tac_calibrate(const uint16_t* Z_fp, const uint16_t* Z_q, int32_t N, int32_t 
  *      allowed.
  *   pos  [T] int32 positions, any sign; NULL: the token's index.
  *   freq [rot / 2] fp64, radians per position: sq_rope_frequencies or one's own.
- *   D % 16 == 0, 16 <= D <= 1024; rot even, 2 <= rot <= D; T H D < 2^35.
+ *   D % 16 == 0, 16 <= D <= 1024; rot even, 2 <= rot <= D; T H D < 2^33.
  *
  * sq_rope_frequencies fills freq with base^(-2 j / rot), scaled for contexts
  * `factor` >= 1 times the original:
@@ -406,7 +406,8 @@ int sq_rope(const uint16_t* X, int64_t x_token, int64_t x_head, const int32_t* p
  *          length are not read.
  * The three live on the device, where no check of them is possible before a launch:
  * rows are clamped to 0 .. T and lengths to 0 .. max_pages page, so no value of them
- * reads or writes outside the tensors.  max_pages page <= 2^28, T <= 2^24.
+ * reads or writes outside the tensors.  max_pages page <= 2^28, T <= 2^24,
+ * B <= 2^14.
  *
  * kv_append writes the new tokens' keys, rotated if freq is given (rotation as
  * sq_rope's, quantised from fp32), and values into the pages, and, if Q is given,
@@ -416,11 +417,14 @@ int sq_rope(const uint16_t* X, int64_t x_token, int64_t x_head, const int32_t* p
  *   rint(code s_old / s_new).  Calling it again with the same arguments changes
  *   nothing.  Codes of slots from the length on keep their bytes.  New tokens
  *   before position 0 (a length shorter than their number) are dropped.  No two
- *   sequences of a call may write the same page.
+ *   table entries that a call writes through may name the same page (several
+ *   sequences may read one).
  *   K, V [T][heads][dim] and Q, Qr [T][Hq][dim] fp16 with strides as in sq_rope;
  *   Qr may be Q with the same strides.
  *   pos  [T] int32 rotary positions; NULL: the cache positions.
- *   (T / page + 2 B) heads + T Hq dim / 4096 < 2^24.
+ *   (T / page + 2 B) heads + T Hq dim / 4096 < 2^24 (/ 512 if rot % 16 != 0).
+ *   Keys and values are finite; what a NaN or an infinity becomes is not defined,
+ *   in its page and head, and nowhere else.
  * kv_read: the listed pages as values code scale, rounded to fp16: K and V
  *   [n][heads][page][dim]; zeros for an entry that is no page.  n heads < 2^24.
  */
@@ -449,11 +453,14 @@ int kv_read(const sq_kv_cache* cache, const int32_t* list, int32_t n, uint16_t* 
  *   cores, scales and softmax in fp32; the softmax weights times their value scale
  *   are rounded to fp16 (2^-11 relative) for the second product, summed in fp32, and
  *   the result is rounded once to fp16.
- *   Q    [T][Hq][dim] fp16, strides as in sq_rope.   O out [T][Hq][dim] fp16, dense.
+ *   Q    [T][Hq][dim] fp16, strides as in sq_rope.   O out [T][Hq][dim] fp16, dense,
+ *        overlapping neither Q nor the cache.
  *   lse  out [T][Hq] fp32, the natural logarithm of the softmax's sum, or NULL.
  *   ws   device workspace of at least sq_attn_kv8_workspace_bytes() for the same
  *        sizes, max_len = max_pages page.  Its contents need no preparation; two
  *        calls that may run at the same time need one each.
+ *   A NaN or an infinity in a query spoils that query's row alone.
+ *   T Hq / 16 + B heads < 2^23; T Hq (Hq / heads) B (max_pages page + 64) < 2^63.
  */
 size_t sq_attn_kv8_workspace_bytes(int32_t T, int32_t B, int32_t Hq, int32_t heads, int32_t dim, int32_t max_len);
 int attn_kv8(const uint16_t* Q, int64_t q_token, int64_t q_head, const sq_kv_cache* cache, const int32_t* cu,
@@ -470,7 +477,7 @@ int attn_kv8(const uint16_t* Q, int64_t q_token, int64_t q_head, const sq_kv_cac
  *     W [N][K] fp16 in; Wq [N][K/2] packed int4 out, s_w [K / group][N] fp16 out.
  *   w4a16_gemm_frag: Y[m][n] = fp16(sum_G s_w[G][n] sum_{k in G} X[m][k] q[n][k]),
  *     sums in fp32, each group's scale applied to its fp32 sum.  X [M][K] fp16, Wf
- *     from sq_weights_to_frag, Y out [M][N] fp16.  Any M; made for few rows, past
+ *     from sq_weights_to_frag, Y out [M][N] fp16 (must not overlap X).  Any M; made for few rows, past
  *     which w4a4_gemm_frag on quantised activations is the faster product.
  *   group: 32, 64 or a multiple of 128, dividing K.  N % 8 == 0.
  */

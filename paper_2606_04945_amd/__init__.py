@@ -519,8 +519,9 @@ def rope(X: torch.Tensor, freq: torch.Tensor, pos: Optional[torch.Tensor] = None
     _need(freq, "freq", torch.float64, (freq.numel(),))
     _need(pos, "pos", torch.int32, (T,), optional=True)
     if out is None:
-        out = torch.empty((T, H, D), dtype=torch.float16, device=X.device)
-    ys = _heads(out, "out", (T, H, D))
+        out, ys = X.new_empty((T, H, D)), (H * D, D)
+    else:
+        ys = _heads(out, "out", (T, H, D))
     _run(lib().sq_rope, (X, freq, pos, out),
          (_ptr(X), *xs, _ptr(pos), _ptr(freq), T, H, D, 2 * freq.numel(), _choice(ROPE_LAYOUTS, layout, "layout"),
           int(transpose), amplitude, _ptr(out), *ys), stream)
@@ -589,8 +590,9 @@ def kv_append(cache: KVCache, K: torch.Tensor, V: torch.Tensor, cu: torch.Tensor
         Hq = q.shape[1]
         qs = _heads(q, "q", (T, Hq, c.dim))
         if q_out is None:
-            q_out = torch.empty((T, Hq, c.dim), dtype=torch.float16, device=q.device)
-        rs = _heads(q_out, "q_out", (T, Hq, c.dim))
+            q_out, rs = q.new_empty((T, Hq, c.dim)), (Hq * c.dim, c.dim)
+        else:
+            rs = _heads(q_out, "q_out", (T, Hq, c.dim))
     else:
         q_out = None
     _run(lib().kv_append, (*cache, K, V, cu, lens, table, pos, freq, q, q_out),
@@ -607,11 +609,13 @@ def kv_read(cache: KVCache, pages: torch.Tensor, *, K=None, V=None, stream=None)
     _need(pages, "pages", torch.int32, (pages.numel(),))
     shape = (pages.numel(), c.heads, c.page, c.dim)
     if K is None:
-        K = torch.empty(shape, dtype=torch.float16, device=pages.device)
+        K = pages.new_empty(shape, dtype=torch.float16)
+    else:
+        _need(K, "K", torch.float16, shape)
     if V is None:
-        V = torch.empty(shape, dtype=torch.float16, device=pages.device)
-    _need(K, "K", torch.float16, shape)
-    _need(V, "V", torch.float16, shape)
+        V = pages.new_empty(shape, dtype=torch.float16)
+    else:
+        _need(V, "V", torch.float16, shape)
     _run(lib().kv_read, (*cache, pages, K, V), (c, _ptr(pages), shape[0], _ptr(K), _ptr(V)), stream)
     return K, V
 
@@ -633,11 +637,15 @@ def attn_kv8(q: torch.Tensor, cache: KVCache, cu: torch.Tensor, lens: torch.Tens
     T, Hq = q.shape[:2]
     qs = _heads(q, "q", (T, Hq, c.dim))
     if out is None:
-        out = torch.empty((T, Hq, c.dim), dtype=torch.float16, device=q.device)
-    if lse is None and want_lse:
-        lse = torch.empty((T, Hq), dtype=torch.float32, device=q.device)
-    _need(out, "out", torch.float16, (T, Hq, c.dim))
-    _need(lse, "lse", torch.float32, (T, Hq), optional=True)
+        out = q.new_empty((T, Hq, c.dim))
+    else:
+        _need(out, "out", torch.float16, (T, Hq, c.dim))
+    if lse is not None:
+        _need(lse, "lse", torch.float32, (T, Hq))
+    elif want_lse:
+        lse = q.new_empty((T, Hq), dtype=torch.float32)
+    if ws is not None:
+        _need(ws, "ws", torch.uint8)
     ws, wsb = _ws(attn_kv8_workspace_bytes(T, B, Hq, c.heads, c.dim, max_pages * c.page), ws, q.device)
     _run(lib().attn_kv8, (q, *cache, cu, lens, table, out, lse, ws),
          (_ptr(q), *qs, c, _ptr(cu), _ptr(lens), _ptr(table), T, B, max_pages, Hq, int(causal), window,
@@ -676,7 +684,8 @@ def w4a16_gemm_frag(X: torch.Tensor, Wf: torch.Tensor, s_w: torch.Tensor, *, Y=N
     _need(Wf, "Wf", torch.uint8, _frag_shape(N, K, 4))
     _need(s_w, "s_w", torch.float16, (ng, N))
     if Y is None:
-        Y = torch.empty((M, N), dtype=torch.float16, device=X.device)
-    _need(Y, "Y", torch.float16, (M, N))
+        Y = X.new_empty((M, N))
+    else:
+        _need(Y, "Y", torch.float16, (M, N))
     _run(lib().w4a16_gemm_frag, (X, Wf, s_w, Y), (_ptr(X), _ptr(Wf), _ptr(s_w), M, N, K, K // ng, _ptr(Y)), stream)
     return Y

@@ -527,6 +527,7 @@ bool aligned4(const void* p) { return ((uintptr_t)p & 3u) == 0; }
 
 constexpr int32_t kMaxTokens = 1 << 24, kMaxPositions = 1 << 28;
 constexpr int64_t kMaxBlocks = 1 << 24;      // workgroups of 256 threads that one launch's grid holds
+constexpr int32_t kMaxSequences = 1 << 14;   // every workgroup looks through them, 64 at a time
 
 // Strides of a [T][H][D] tensor, dense in D; those of an extent of one do not count.
 int check_strides(int64_t token, int64_t head, int32_t T, int32_t H, int32_t D, bool out, const char* name,
@@ -567,8 +568,8 @@ int check_cache(const sq_kv_cache* c, const char* name) {
 
 int check_batch(const sq_kv_cache* c, const int32_t* cu, const int32_t* lens, const int32_t* table, int32_t T,
                 int32_t B, int32_t max_pages, const char* name) {
-    SQ_REQUIRE(T >= 0 && T <= kMaxTokens && B >= 0, SQ_ERR_SHAPE, "%s: T=%d B=%d: need 0 <= T <= %d, B >= 0", name, T,
-               B, kMaxTokens);
+    SQ_REQUIRE(T >= 0 && T <= kMaxTokens && B >= 0 && B <= kMaxSequences, SQ_ERR_SHAPE,
+               "%s: T=%d B=%d: need 0 <= T <= %d, 0 <= B <= %d", name, T, B, kMaxTokens, kMaxSequences);
     SQ_REQUIRE(max_pages >= 0 && (int64_t)max_pages * c->page <= kMaxPositions, SQ_ERR_SHAPE,
                "%s: max_pages=%d: need at most %d positions", name, max_pages, kMaxPositions);
     if (T == 0 || B == 0) return SQ_OK;
@@ -621,7 +622,7 @@ int sq_rope(const uint16_t* X, int64_t x_token, int64_t x_head, const int32_t* p
     SQ_REQUIRE(D >= 16 && D <= 1024 && D % 16 == 0, SQ_ERR_SHAPE, "sq_rope: D=%d: need a multiple of 16 in 16 .. 1024",
                D);
     SQ_TRY(check_rotation(rot, layout, amplitude, D, "sq_rope"));
-    SQ_REQUIRE(T >= 0 && H >= 0 && (double)T * H * D < 0x1p35, SQ_ERR_SHAPE, "sq_rope: T=%d H=%d: need T H D < 2^35", T,
+    SQ_REQUIRE(T >= 0 && H >= 0 && (double)T * H * D < 0x1p33, SQ_ERR_SHAPE, "sq_rope: T=%d H=%d: need T H D < 2^33", T,
                H);
     if (T == 0 || H == 0) return SQ_OK;
     SQ_TRY(check_strides(x_token, x_head, T, H, D, false, "sq_rope", "X"));
@@ -647,7 +648,8 @@ int kv_append(const sq_kv_cache* cache, const uint16_t* K, int64_t k_token, int6
     if (freq) SQ_TRY(check_rotation(rot, layout, amplitude, c.dim, "kv_append"));
     SQ_REQUIRE(!Q || (freq && Qr), SQ_ERR_NULL, "kv_append: Q needs freq and Qr");
     SQ_REQUIRE(!Q || (Hq >= 1 && Hq <= 1024), SQ_ERR_SHAPE, "kv_append: Hq=%d: need 1 .. 1024", Hq);
-    SQ_REQUIRE(((int64_t)T / c.page + 2 * (int64_t)B) * c.heads + (Q ? (int64_t)T * Hq * c.dim / 4096 : 0) < kMaxBlocks,
+    const int64_t per = freq && rot % 16 ? 512 : 4096;       // entries of Q that a workgroup rotates, at least
+    SQ_REQUIRE(((int64_t)T / c.page + 2 * (int64_t)B) * c.heads + (Q ? (int64_t)T * Hq * c.dim / per : 0) < kMaxBlocks,
                SQ_ERR_SHAPE, "kv_append: T=%d B=%d: too many rows for one call", T, B);
     if (T == 0 || B == 0) return SQ_OK;
     SQ_TRY(check_strides(k_token, k_head, T, c.heads, c.dim, false, "kv_append", "K"));
@@ -695,8 +697,10 @@ int attn_kv8(const uint16_t* Q, int64_t q_token, int64_t q_head, const sq_kv_cac
     SQ_TRY(check_batch(cache, cu, lens, table, T, B, max_pages, "attn_kv8"));
     SQ_REQUIRE(Hq >= 1 && Hq <= 1024 && Hq % c.heads == 0, SQ_ERR_SHAPE,
                "attn_kv8: Hq=%d: need a multiple of heads=%d, at most 1024", Hq, c.heads);
-    SQ_REQUIRE((int64_t)T * Hq / 16 + (int64_t)B * c.heads < kMaxBlocks, SQ_ERR_SHAPE,
-               "attn_kv8: T=%d B=%d: too many rows for one call", T, B);
+    // workgroups of up to 512 threads; and sums of weights stay below 2^63, whatever cu holds
+    SQ_REQUIRE((int64_t)T * Hq / 16 + (int64_t)B * c.heads < kMaxBlocks / 2 &&
+                   (double)T * Hq * (Hq / c.heads) * B * ((double)max_pages * c.page + 64) < 0x1p63,
+               SQ_ERR_SHAPE, "attn_kv8: T=%d B=%d max_pages=%d: too much for one call", T, B, max_pages);
     SQ_REQUIRE(window >= 0, SQ_ERR_SHAPE, "attn_kv8: window=%d < 0", window);
     SQ_REQUIRE(isfinite(scale), SQ_ERR_SHAPE, "attn_kv8: the scale is not finite");
     if (T == 0 || B == 0) return SQ_OK;
@@ -704,6 +708,7 @@ int attn_kv8(const uint16_t* Q, int64_t q_token, int64_t q_head, const sq_kv_cac
     SQ_REQUIRE(Q && O, SQ_ERR_NULL, "attn_kv8: Q and O are required");
     SQ_REQUIRE(aligned16(Q) && aligned16(O) && aligned16(lse) && aligned16(ws), SQ_ERR_ALIGN,
                "attn_kv8: pointers must be 16-byte aligned");
+    SQ_REQUIRE(Q != O, SQ_ERR_SHAPE, "attn_kv8: O must not overlap Q");
     const size_t need = sq_attn_kv8_workspace_bytes(T, B, Hq, c.heads, c.dim, max_pages * c.page);
     SQ_REQUIRE(ws_bytes >= need && (need == 0 || ws), SQ_ERR_WORKSPACE, "attn_kv8: workspace %zu B < %zu B", ws_bytes,
                need);
@@ -736,6 +741,7 @@ int w4a16_gemm_frag(const uint16_t* X, const uint8_t* Wf, const uint16_t* s_w, i
     SQ_REQUIRE(X && Wf && s_w && Y, SQ_ERR_NULL, "w4a16_gemm_frag: X, Wf, s_w and Y are required");
     SQ_REQUIRE(aligned16(X) && aligned16(Wf) && aligned16(s_w) && aligned16(Y), SQ_ERR_ALIGN,
                "w4a16_gemm_frag: pointers must be 16-byte aligned");
+    SQ_REQUIRE(X != Y, SQ_ERR_SHAPE, "w4a16_gemm_frag: Y must not overlap X");
     return hip_status(sq::launch_w4a16_frag(X, Wf, s_w, M, N, K, group, Y, static_cast<hipStream_t>(stream)),
                       "w4a16_gemm_frag");
 }

@@ -281,7 +281,7 @@ __device__ __forceinline__ void store_result(uint16_t* o, f4 x, float inv) {
 }
 
 __device__ __forceinline__ float result_lse(float m, float l) {
-    return l > 0.0f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : kNone;
+    return l == 0.0f ? kNone : (m + __builtin_amdgcn_logf(l)) * kLn2;      // NaN of a NaN
 }
 
 }  // namespace

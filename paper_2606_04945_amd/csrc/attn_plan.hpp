@@ -45,7 +45,7 @@ struct AttnSeq {
 SQ_HD AttnSeq attn_seq(const AttnShape& a, int c0, int c1, int len) {
     AttnSeq q;
     q.s = make_seq(c0, c1, len, a.T, a.max_len);
-    q.tiles = (q.s.n * a.G + a.rows - 1) / a.rows;      // T G is below 2^28
+    q.tiles = (q.s.n * a.G + a.rows - 1) / a.rows;      // T G is below 2^27
     if (a.causal && !a.window) {
         q.slope = a.rows;
         q.base = (int64_t)a.G * ((q.s.off > 0 ? q.s.off : 0) + kAttnStep) + a.rows;

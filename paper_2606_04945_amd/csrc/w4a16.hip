@@ -123,9 +123,12 @@ __global__ __launch_bounds__(TM == 4 ? 256 : 512) void w4a16_kernel(const uint16
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
-            for (int s = 0; s < 4; ++s)
+            for (int s = 0; s < 4; ++s) {
+                // (an offset in the scalar part that passes the buffer would undo the check of the other)
+                const bool some = !kEdge || t * 128 + 32 * s < K;
                 f.x[i][s] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(
-                                rX, (int)(!kEdge || t * 128 + 32 * s < K ? xv[i] : kOOB), at * 256 + 64 * s, 0));
+                                rX, (int)(some ? xv[i] : kOOB), some ? t * 256 + 64 * s : 0, 0));
+            }
     };
     const NibbleMasks masks = nibble_masks();
     f4 sum[NG][TM];

@@ -35,7 +35,7 @@ def test_rope(lib):
     for kw in (dict(D=24), dict(D=0), dict(D=1040, rot=64, xt=2080, yt=2080, yh=1040), dict(rot=0), dict(rot=3),
                dict(rot=66), dict(layout=2), dict(layout=-1), dict(amp=NAN), dict(amp=INF), dict(T=-1), dict(H=-1),
                dict(xt=129), dict(xh=-64), dict(yt=64), dict(yh=32), dict(yt=8, yh=64),
-               dict(T=1 << 24, H=1024, D=64), dict(Y=FAKE, yt=256)):
+               dict(T=1 << 24, H=1024, D=64), dict(T=1 << 20, H=128, D=64, xh=64, xt=8192, yt=8192), dict(Y=FAKE, yt=256)):
         assert rope(lib, **kw) == L.SQ_ERR_SHAPE, kw
     for kw in (dict(X=None), dict(Y=None), dict(freq=None)):
         assert rope(lib, **kw) == L.SQ_ERR_NULL, kw
@@ -76,7 +76,8 @@ def test_append(lib):
     assert append(lib, dict(v=BAD)) == L.SQ_ERR_ALIGN
     for kw in (dict(T=-1), dict(T=(1 << 24) + 1), dict(B=-1), dict(mp=-1), dict(mp=(1 << 22) + 1), dict(rot=65),
                dict(rot=66), dict(layout=2), dict(amp=NAN), dict(Hq=0), dict(Hq=1025), dict(kt=12), dict(vh=-8),
-               dict(qt=4), dict(rt=64), dict(rh=8), dict(R=FAKE, rt=512), dict(B=1 << 22), dict(T=1 << 24, Hq=1024)):
+               dict(qt=4), dict(rt=64), dict(rh=8), dict(R=FAKE, rt=512), dict(B=(1 << 14) + 1),
+               dict(T=1 << 24, Hq=1024), dict(B=1 << 14, c=dict(heads=512)), dict(T=1 << 24, Hq=16, rot=2)):
         assert append(lib, **kw) == L.SQ_ERR_SHAPE, kw
     for kw in (dict(K=None), dict(V=None), dict(cu=None), dict(lens=None), dict(table=None), dict(R=None),
                dict(freq=None)):
@@ -106,7 +107,7 @@ def test_read(lib):
 
 def attn(lib, c=None, **kw):
     a = dict(Q=FAKE, qt=256, qh=64, c=cache(**(c or {})), cu=FAKE, lens=FAKE, table=FAKE, T=4, B=2, mp=3, Hq=4, causal=1,
-             window=0, scale=0.125, O=FAKE, lse=None, ws=FAKE, wsb=1 << 30)
+             window=0, scale=0.125, O=FAKE << 1, lse=None, ws=FAKE, wsb=1 << 30)
     a.update(kw)
     return lib.attn_kv8(*a.values(), None)
 
@@ -118,7 +119,8 @@ def test_attention(lib):
         assert attn(lib, c) == L.SQ_ERR_NULL, c
     for kw in (dict(T=-1), dict(T=(1 << 24) + 1), dict(B=-1), dict(mp=-1), dict(mp=(1 << 22) + 1), dict(Hq=0),
                dict(Hq=3), dict(Hq=1026), dict(window=-1), dict(scale=NAN), dict(scale=INF), dict(qt=100), dict(qh=-64),
-               dict(B=1 << 23), dict(T=1 << 24, Hq=32)):
+               dict(B=(1 << 14) + 1), dict(T=1 << 24, Hq=32), dict(B=1 << 14, c=dict(heads=512), Hq=512),
+               dict(T=1 << 17, B=1 << 14, Hq=512, mp=1 << 22), dict(O=FAKE)):
         assert attn(lib, **kw) == L.SQ_ERR_SHAPE, kw
     for kw in (dict(Q=None), dict(O=None), dict(cu=None), dict(lens=None), dict(table=None)):
         assert attn(lib, **kw) == L.SQ_ERR_NULL, kw
@@ -147,6 +149,7 @@ def test_weight_only(lib):
     assert g(FAKE, FAKE, FAKE, -1, 8, 128, 32, FAKE, None) == L.SQ_ERR_SHAPE
     assert g(FAKE, FAKE, FAKE, 1 << 21, 8, 128, 32, FAKE, None) == L.SQ_ERR_SHAPE
     assert g(FAKE, FAKE, FAKE, 1, 1 << 20, 8192, 32, FAKE, None) == L.SQ_ERR_SHAPE      # 4 GiB of codes
+    assert g(FAKE, FAKE, FAKE, 1, 8, 128, 32, FAKE, None) == L.SQ_ERR_SHAPE              # Y on X
     assert g(FAKE, None, FAKE, 1, 8, 128, 32, FAKE, None) == L.SQ_ERR_NULL
     assert g(FAKE, FAKE, FAKE + 8, 1, 8, 128, 32, FAKE, None) == L.SQ_ERR_ALIGN
     assert g(None, None, None, 0, 8, 128, 32, None, None) == L.SQ_OK
