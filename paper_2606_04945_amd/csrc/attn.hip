@@ -7,30 +7,50 @@ namespace {
 
 // Joins the partial results of the tiles that workers share:
 //   out = sum_i 2^(m_i - M) O_i / sum_i 2^(m_i - M) l_i.
-// A workgroup looks at `each` workers' records and joins `share` rows of the tiles it
-// finds there.  A group of D / 4 threads has a row, four channels a thread; where a tile
-// has more groups than rows, several share a row's results and meet in LDS in order.
-// Which worker ended first changes nothing.
+// Every workgroup finds the shared tiles in the workers' entries; tiles times parts of
+// their rows go round the workgroups, as many parts as make that one each, so that a few
+// tiles of many results and many of few both spread over the card.  A group of D / 4
+// threads has a row, four channels a thread; where a workgroup has more groups than rows,
+// several share a row's results and meet in LDS in order.  Which worker ended first
+// changes nothing.
 constexpr int kJoinThreads = 256, kJoinGroups = 64;    // at most: heads of 16
-__global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(AttnArgs p, int each, int share) {
+constexpr int kJoinBlocks = 512, kJoinMasks = kAttnCus * 8 / kWave;
+__global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(AttnArgs p) {
+    __shared__ uint64_t masks[kJoinMasks];
     __shared__ float ml[2 * kJoinGroups];
     __shared__ f4 part[kJoinThreads];
     const int tid = threadIdx.x, R = p.a.rows, D = p.D, G = p.a.G;
     const int vecs = D / 4, groups = kJoinThreads / vecs, gi = tid / vecs, v = tid % vecs;
-    const int first = blockIdx.x * each, row0 = blockIdx.y * share;
+    const int lane = tid % kWave, wave = tid / kWave;
     const int64_t size = attn_place_floats(R, D);
-    // a wave's lanes look at the records together
-    const int lane = tid % kWave, mine = first + lane;
-    const int last = lane < each && mine < p.a.workers ? p.records[mine].last : -1;
-    for (uint64_t found = __ballot(last >= 0); found; found &= found - 1) {
-        const int w0 = first + __builtin_ctzll(found), n = __builtin_amdgcn_readlane(last, w0 - first) - w0 + 1;
+    // 64 workers a mask, a bit each: a tile that others end
+    int last[kJoinMasks / 4];
+#pragma unroll
+    for (int i = 0; i < kJoinMasks / 4; ++i) last[i] = p.lasts[min(i * kJoinThreads + tid, p.a.workers - 1)];
+    if (!*p.shared) return;
+#pragma unroll
+    for (int i = 0; i < kJoinMasks / 4; ++i) {
+        const uint64_t found = __ballot(i * kJoinThreads + tid < p.a.workers && last[i] >= 0);
+        if (lane == 0) masks[i * 4 + wave] = found;
+    }
+    __syncthreads();
+    const uint64_t mask = lane < kJoinMasks ? masks[lane] : 0;
+    const int upto = (int)wave_scan(__popcll(mask)), tiles = __builtin_amdgcn_readlane(upto, kWave - 1);
+    if (tiles == 0) return;
+    const int parts = min(R, max(1, kJoinBlocks / tiles));
+    for (int item = blockIdx.x; item < tiles * parts; item += kJoinBlocks) {
+        const int k = item / parts, first = item % parts;      // rows first, first + parts, ...
+        const int at_mask = __builtin_ctzll(__ballot(upto > k));
+        uint64_t bits = (uint64_t)lane_value((int64_t)mask, at_mask);
+        for (int z = k - (__builtin_amdgcn_readlane(upto, at_mask) - __popcll(bits)); z > 0; --z) bits &= bits - 1;
+        const int w0 = at_mask * kWave + __builtin_ctzll(bits), n = p.lasts[w0] - w0 + 1;
         const AttnRecord t = p.records[w0];
-        const int rows = min(min(R, row0 + share), t.rows - t.row0);
-        if (row0 >= rows) continue;
-        const int per = min(n, max(1, groups / (rows - row0)));          // groups of threads to a row
-        for (int r0 = row0; r0 < rows; r0 += groups / per) {
-            const int row = r0 + gi / per;
-            const bool in = gi < groups / per * per && row < rows;
+        const int rows = (min(R, t.rows - t.row0) - first + parts - 1) / parts;
+        if (rows <= 0) continue;
+        const int per = min(n, max(1, groups / rows));         // groups of threads to a row
+        for (int r0 = 0; r0 < rows; r0 += groups / per) {
+            const int row = first + (r0 + gi / per) * parts;
+            const bool in = gi < groups / per * per && r0 + gi / per < rows;
             float m = kNone, l = 0.0f;
             f4 O{0, 0, 0, 0};
             if (in) {
@@ -100,16 +120,14 @@ hipError_t launch_attn(const uint16_t* Q, int64_t q_token, int64_t q_head, const
                        const int32_t* cu, const int32_t* lens, const int32_t* table, int T, int B, int max_pages, int Hq,
                        bool causal, int window, float scale, uint16_t* O, float* lse, void* ws, hipStream_t st) {
     const AttnShape a = attn_shape(T, B, Hq, heads, D, max_pages * page, causal, window);
-    AttnRecord* records = static_cast<AttnRecord*>(ws);
+    int *shared = static_cast<int*>(ws), *lasts = shared + 4;
+    AttnRecord* records = reinterpret_cast<AttnRecord*>(lasts + a.workers);
     const AttnArgs p{a, Q, q_token, q_head, k, v, k_scale, v_scale, pages, page, __builtin_ctz((unsigned)page), D,
                      cu, lens, table, max_pages, fabsf(scale) * kLog2e, scale < 0.0f ? 0x80008000u : 0u, O, lse,
-                     records, reinterpret_cast<float*>(records + a.workers)};
+                     shared, lasts, records, reinterpret_cast<float*>(records + a.workers)};
     const hipError_t e = a.rows > 32 ? launch_attn_tile(p, st) : launch_attn_wave(p, st);
     if (e != hipSuccess || attn_always_direct(a)) return e;
-    // about 2048 workgroups: few long lists of results (a row each) or many short ones
-    const int each = a.rows > 32 ? 1 : 16, share = a.rows > 32 ? 32 : 1;
-    hipLaunchKernelGGL(attn_join_kernel, dim3((unsigned)((a.workers + each - 1) / each), (unsigned)(a.rows / share)),
-                       dim3(kJoinThreads), 0, st, p, each, share);
+    hipLaunchKernelGGL(attn_join_kernel, dim3(kJoinBlocks), dim3(kJoinThreads), 0, st, p);
     return hipGetLastError();
 }
 

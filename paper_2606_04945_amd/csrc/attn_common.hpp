@@ -34,7 +34,8 @@ struct AttnArgs {
     uint32_t flip;                  // sign bits of a pair of halves where the scale is negative
     uint16_t* O;
     float* lse;
-    AttnRecord* records;            // of the workspace, and its places
+    int *shared, *lasts;            // of the workspace: whether tiles are shared; a worker's last worker,
+    AttnRecord* records;            // its record, its places
     float* places;
 };
 
@@ -150,7 +151,9 @@ struct Share {
 };
 __device__ __forceinline__ Share find_share(const AttnArgs& p, int64_t total, const Group& first, int worker,
                                             int lane) {
-    const AttnCut cut = attn_cut_work(total, p.a.workers);
+    const int workers = attn_workers(p.a, total);
+    const AttnCut cut = attn_cut_work(total, workers);
+    if (worker >= workers) return {0, 0, 0, p.a.B, cut};
     Share s{attn_start(cut, worker), attn_start(cut, worker + 1), 0, p.a.B, cut};
     for (int b0 = 0; b0 < p.a.B; b0 += kWave) {
         const int64_t w = group_seq(p, b0 ? load_group(p, b0, lane) : first).weight, upto = wave_scan(w);
@@ -195,6 +198,13 @@ __device__ __forceinline__ int xcd_worker(int L, int W) {
     return x * base + (x < rem ? x : rem) + L / kXcds;
 }
 
+// A wave's or a workgroup's worker: runs of them as above, or, where some have no part,
+// the ones that do spread over the workgroups.
+__device__ __forceinline__ int worker_of(const AttnArgs& p, const Survey& all, int wave, int waves) {
+    if (attn_workers(p.a, all.total) < p.a.workers) return wave * p.a.groups + blockIdx.x;
+    return xcd_worker(blockIdx.x, p.a.groups) * waves + wave;
+}
+
 // The tile at a worker's position and what it does of it; moves the position on, and
 // leaves the record of a tile that goes on in a later worker's part.  False at the end.
 struct Tile {
@@ -219,9 +229,8 @@ __device__ __forceinline__ bool next_tile(const AttnArgs& p, const Group& first,
         if (t.part.ends_inside && !t.part.begins_inside) {
             const int64_t past = sh.before + h * q.weight + attn_before(q, r) + q.base + q.slope * r;
             if (threadIdx.x % kWave == 0) {
-                AttnRecord* record = p.records + worker;
-                store_global(record, v4i{attn_worker(sh.cut, past - 1), q.s.t0, q.s.n * p.a.G, r * p.a.rows});
-                store_global(&record->h, h);
+                store_global(p.lasts + worker, attn_worker(sh.cut, past - 1));
+                store_global(p.records + worker, v4i{q.s.t0, q.s.n * p.a.G, r * p.a.rows, h});
             }
         }
         return true;

@@ -93,6 +93,14 @@ SQ_HD AttnSteps attn_steps(const AttnShape& a, const Seq& s, int r) {
     return {lo / kAttnStep, (hi + kAttnStep - 1) / kAttnStep - lo / kAttnStep};
 }
 
+// Workers that get a part: so few that each has two steps, four of tiles of 128 rows,
+// about.  With all of them, however little that leaves each, a batch of few tiles spends
+// its time on partial results: 32 tokens of 8 query heads to 2 key heads over 30000 keys
+// 43 us against 36, of which 11 are the joining.
+SQ_HD int attn_workers(const AttnShape& a, int64_t total) {
+    const int64_t parts = divide(total, (int64_t)a.G * kAttnStep * (a.rows > 32 ? 4 : 2)) + 1;
+    return parts < a.workers ? (int)parts : a.workers;
+}
 // The weight in equal parts: worker w's are positions [attn_start(w), attn_start(w + 1)).
 struct AttnCut {
     int64_t each, more;           // the first `more` workers have one position more
@@ -131,24 +139,22 @@ SQ_HD AttnPart attn_part(const AttnShape& a, const AttnSeq& q, int64_t before, i
     return {from + x1, s.first + k0, s.first + k1, k1 - k0 == s.count && (s.count > 0 || x0 == 0), x0 > 0, x1 < weight};
 }
 
-// The workspace of a batch whose tiles are shared out.  Every worker has a record and
-// two places for partial results: of the tile its part begins inside of, and of the one
-// that begins in its part and ends in a later worker's.  The record is of the second:
-// the joining kernel finds there what to join, from this worker's place for it and the
-// first places of the workers up to `last`; -1: nothing.  A worker that has no step of
-// a tile, or all of them and wrote the rows, leaves its place without a maximum (-inf).
+// The workspace of a batch whose tiles are shared out.  Every worker has two places for
+// partial results: of the tile its part begins inside of, and of the one that begins in
+// its part and ends in a later worker's.  Of the second it leaves the tile's last worker
+// (-1: there is none) and a record: the joining kernel joins this worker's place for it
+// and the first places of the workers up to the last.  A worker that has no step of a
+// tile, or all of them and wrote the rows, leaves its place without a maximum (-inf).
+// A first word says whether tiles are shared at all.
 struct AttnRecord {
-    int last;             // last worker of the tile, or -1
     int t0, rows;         // the sequence's first row of the batch, its rows of a key head
-    int row0;             // the tile's first
-    int h;
-    int unused[3];
+    int row0, h;          // the tile's first row and key head
 };
 SQ_HD int attn_place(int w, bool begins_inside) { return 2 * w + (begins_inside ? 0 : 1); }
 // Per row of a tile: D sums in fp32, the reference and the sum of the row's softmax.
 SQ_HD int64_t attn_place_floats(int rows, int D) { return (int64_t)rows * (D + 2); }
 inline int64_t attn_workspace(const AttnShape& a, int D) {
-    return a.workers * ((int64_t)sizeof(AttnRecord) + 2 * attn_place_floats(a.rows, D) * 4);
+    return 16 + a.workers * (4 + (int64_t)sizeof(AttnRecord) + 2 * attn_place_floats(a.rows, D) * 4);
 }
 
 // Tiles of all sequences and key heads, at most: places in a list where a batch is read

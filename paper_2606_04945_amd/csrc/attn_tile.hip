@@ -59,9 +59,8 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_tile_kernel(AttnA
     const Survey all = survey(p, first, lane);
     Share sh{};
     Tile tile{};
-    const int worker = xcd_worker(blockIdx.x, p.a.groups);
-    if (!attn_always_direct(p.a) && (int)blockIdx.x < p.a.groups && tid == 0)
-        store_global(&p.records[worker].last, -1);
+    const int worker = worker_of(p, all, 0, 1);
+    if (!attn_always_direct(p.a) && blockIdx.x == 0 && threadIdx.x == 0) store_global(p.shared, (int)!all.direct);
     if (all.direct) {
         const int64_t tiles = gridDim.x / p.a.heads;
         const int64_t at = xcd_worker(blockIdx.x, gridDim.x);
@@ -74,6 +73,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_tile_kernel(AttnA
         tile = {l.q.s, l.b, (int)(at / tiles), (int)r64, {0, steps.first, steps.first + steps.count, true, false, false}};
     } else {
         if ((int)blockIdx.x >= p.a.groups) return;
+        if (tid == 0) store_global(p.lasts + worker, -1);
         sh = find_share(p, all.total, first, worker, lane);
     }
     for (;;) {

@@ -268,9 +268,8 @@ __global__ __launch_bounds__(NW* kWave) void attn_wave_kernel(AttnArgs p) {
     Share sh{};
     Tile t{};
     int stride = 1, count = 0;
-    const int worker = xcd_worker(blockIdx.x, p.a.groups) * NW + wave;
-    if (!attn_always_direct(p.a) && (int)blockIdx.x < p.a.groups && lane == 0)
-        store_global(&p.records[worker].last, -1);
+    const int worker = worker_of(p, all, wave, NW);
+    if (!attn_always_direct(p.a) && blockIdx.x == 0 && threadIdx.x == 0) store_global(p.shared, (int)!all.direct);
     if (all.direct) {
         const int64_t item = blockIdx.x / p.a.heads;
         const Listed at = find_listed(p, item, first, lane);
@@ -283,6 +282,7 @@ __global__ __launch_bounds__(NW* kWave) void attn_wave_kernel(AttnArgs p) {
              {0, steps.first + wave, steps.first + steps.count, false, false, false}};
     } else {
         if ((int)blockIdx.x >= p.a.groups) return;
+        if (lane == 0) store_global(p.lasts + worker, -1);
         sh = find_share(p, all.total, first, worker, lane);
     }
     for (;;) {

@@ -38,13 +38,14 @@ extern "C" int walk(int T, int B, int heads, int G, int max_len, int causal, int
     std::map<Tile, std::map<int, bool>> written;           // places: whether they hold a result
     std::map<Tile, int> direct;
     std::set<int> places;
-    std::vector<AttnRecord> records(a.workers);
+    std::vector<int> lasts(a.workers, -1);
+    const int workers = attn_workers(a, total);
+    if (workers < 1 || workers > a.workers) return 24;
     std::vector<Tile> recorded(a.workers);
     int64_t most = 0, least = INT64_MAX;
-    const AttnCut cut = attn_cut_work(total, a.workers);
-    if (attn_start(cut, 0) != 0 || attn_start(cut, a.workers) != total) return 16;
-    for (int w = 0; w < a.workers; ++w) {
-        records[w].last = -1;
+    const AttnCut cut = attn_cut_work(total, workers);
+    if (attn_start(cut, 0) != 0 || attn_start(cut, workers) != total) return 16;
+    for (int w = 0; w < workers; ++w) {
         int64_t at = attn_start(cut, w), end = attn_start(cut, w + 1), did = 0;
         if (end < at) return 4;
         int b = 0;
@@ -62,10 +63,10 @@ extern "C" int walk(int T, int B, int heads, int G, int max_len, int causal, int
             if (part.begins_inside != (at > from) || part.ends_inside != (part.next < from + weight)) return 18;
             const Tile t(b, h, r);
             if (part.ends_inside && !part.begins_inside) {
-                if (records[w].last >= 0) return 19;
-                records[w] = {attn_worker(cut, from + weight - 1), q.s.t0, q.s.n * G, r * rows, h, {0, 0, 0}};
+                if (lasts[w] >= 0) return 19;
+                lasts[w] = attn_worker(cut, from + weight - 1);
                 recorded[w] = t;
-                if (records[w].last <= w || records[w].last >= a.workers) return 20;
+                if (lasts[w] <= w || lasts[w] >= workers) return 20;
             }
             at = part.next;
             const AttnSteps st = attn_steps(a, q.s, r);
@@ -87,10 +88,10 @@ extern "C" int walk(int T, int B, int heads, int G, int max_len, int causal, int
     }
     int64_t slots = attn_tile_slots(a);
     std::map<Tile, int> joined;
-    for (int w = 0; w < a.workers; ++w)
-        if (records[w].last >= 0) {
+    for (int w = 0; w < workers; ++w)
+        if (lasts[w] >= 0) {
             std::map<int, bool> join;
-            for (int j = w; j <= records[w].last; ++j) {
+            for (int j = w; j <= lasts[w]; ++j) {
                 const int place = attn_place(j, j > w);
                 if (!written[recorded[w]].count(place)) return 22;
                 join[place] = written[recorded[w]][place];
