@@ -11,7 +11,7 @@
 #include <mutex>
 
 #include "../../include/starquant.h"
-#include "sq_internal.hpp"
+#include "serve.hpp"
 
 namespace {
 

@@ -179,7 +179,8 @@ __device__ __forceinline__ Listed find_listed(const AttnArgs& p, int64_t item, c
     Listed r{};
     Group g = first;
     for (int b0 = 0;;) {
-        const bool at = b0 + lane < p.a.B && list_start(min(max(g.c0, 0), p.a.T), b0 + lane, p.a.G, p.a.rows, 1) <= item;
+        const int64_t start = list_start(min(max(g.c0, 0), p.a.T), b0 + lane, p.a.G, p.a.rows, 1);
+        const bool at = b0 + lane < p.a.B && start <= item;
         const int n = __popcll(__ballot(at));
         if (n > 0) {
             r.b = b0 + n - 1;

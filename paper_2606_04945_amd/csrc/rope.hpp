@@ -8,7 +8,7 @@
 // formed and reduced in fp64 and only what is left of it, at most half a turn,
 // goes to fp32.
 #pragma once
-#include "sq_internal.hpp"
+#include "serve.hpp"
 
 namespace sq {
 

@@ -8,6 +8,7 @@
 // byte is read once.  Codes become halves in registers (exact), the fp16 matrix
 // cores sum a group's products in fp32, and the group's scale is applied to that
 // fp32 sum.
+#include "serve.hpp"
 #include "tile_common.hpp"
 #include "w4a16_plan.hpp"
 
@@ -81,9 +82,10 @@ struct Step {
 // matrix instruction takes all its inputs from one such group instead, so that it
 // never mixes scales: four lane-row exchanges per 32 codes.
 template <int TM, int NG, int GROUP>
-__global__ __launch_bounds__(TM == 4 ? 256 : 512) void w4a16_kernel(const uint16_t* __restrict__ X, const uint8_t* __restrict__ Wf,
-                                                    const uint16_t* __restrict__ s_w, int M, int N, int K, int group,
-                                                    uint16_t* __restrict__ Y) {
+__global__ __launch_bounds__(TM == 4 ? 256 : 512) void w4a16_kernel(const uint16_t* __restrict__ X,
+                                                                    const uint8_t* __restrict__ Wf,
+                                                                    const uint16_t* __restrict__ s_w, int M, int N,
+                                                                    int K, int group, uint16_t* __restrict__ Y) {
     extern __shared__ __attribute__((aligned(16))) uint8_t sm[];
     constexpr int CH = 128 / GROUP, PER = 4 / CH;      // scales a step, matrix instructions a scale
     const int waves = blockDim.x / kWave;
