@@ -277,10 +277,12 @@ __device__ __forceinline__ BlockScale block_scale(bool in, float ks, float vs, f
     return {in ? k : 0.0f, in ? __builtin_amdgcn_logf(s) : kNone, in ? 1.0f / s : 0.0f};
 }
 
+__device__ __forceinline__ h8 load_query(const uint16_t* q) {
+    return __builtin_bit_cast(h8, *reinterpret_cast<const v4i*>(q));
+}
 // a negative scale's sign goes into the queries, so that larger products are larger logits
-__device__ __forceinline__ h8 load_query(const uint16_t* q, uint32_t flip) {
-    const v4i x = *reinterpret_cast<const v4i*>(q);
-    return __builtin_bit_cast(h8, x ^ (int)flip);
+__device__ __forceinline__ h8 flip_query(h8 q, uint32_t flip) {
+    return __builtin_bit_cast(h8, __builtin_bit_cast(v4i, q) ^ (int)flip);
 }
 
 // four results of a row as fp16

@@ -187,10 +187,27 @@ SQ_HD bool attn_direct(const AttnShape& a, int64_t total, int64_t most) {
 // more than 64 (4 x 1024 tokens 266 / - / 199).
 constexpr int kAttnCus = 256;
 
+// Tiles of 128 rows read tile by tile: a head's tiles run on as few XCDs as share it,
+// which read the same keys, and go round them one by one, so that each has its share of
+// long sequences; the longest tiles of a sequence first.  Both together: 14 x 400 .. 862
+// tokens over 4000 keys 583 -> 536 us, over 1000 225 -> 212, 8 prompts of up to 2048 411
+// -> 400; either alone gains less than half of that.
+SQ_HD int attn_head_xcds(int heads) {
+    const int low = heads & -heads;                     // 8 XCDs
+    return low >= 8 ? 1 : 8 / low;
+}
+// Place `at` of a head's list, in which every XCD has a run of tiles / xcds: its tile.
+SQ_HD int64_t attn_spread(int64_t at, int64_t tiles, int xcds) {
+    const int64_t run = tiles / xcds;
+    return at % run * xcds + at / run;
+}
+
 // Workgroups: a place for every tile, and those that share the work.
 inline int64_t attn_grid(const AttnShape& a) {
-    const int64_t tiles = attn_tile_slots(a);
-    return attn_always_direct(a) || tiles > a.groups ? tiles : a.groups;
+    int64_t n = attn_tile_slots(a);
+    if (!attn_always_direct(a) && n < a.groups) n = a.groups;
+    const int64_t whole = a.heads * (a.rows > 32 ? attn_head_xcds(a.heads) : 1);
+    return (n + whole - 1) / whole * whole;
 }
 
 // Waves of a workgroup that reads with single waves: what its registers hold without

@@ -71,13 +71,14 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_tile_kernel(AttnA
     if (all.direct) {
         const int64_t tiles = gridDim.x / p.a.heads;
         const int64_t at = xcd_worker(blockIdx.x, gridDim.x);
-        const int64_t item = at % tiles;               // a head's tiles run on one XCD
+        const int64_t item = attn_spread(at % tiles, tiles, attn_head_xcds(p.a.heads));
         if (at / tiles >= p.a.heads) return;
         const Listed l = find_listed(p, item, first, lane);
         const int64_t r64 = item - list_start(l.q.s.t0, l.b, G, R, 1);
         if (r64 < 0 || r64 >= l.q.tiles) return;
-        const AttnSteps steps = attn_steps(p.a, l.q.s, (int)r64);
-        tile = {l.q.s, l.b, (int)(at / tiles), (int)r64,
+        const int r = l.q.tiles - 1 - (int)r64;
+        const AttnSteps steps = attn_steps(p.a, l.q.s, r);
+        tile = {l.q.s, l.b, (int)(at / tiles), r,
                 {0, steps.first, steps.first + steps.count, true, false, false}};
     } else {
         if ((int)blockIdx.x >= p.a.groups) return;
@@ -105,7 +106,8 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_tile_kernel(AttnA
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
             const int d = 16 * s + 8 * half;
-            Q[s] = d < D ? load_query(p.Q + t * p.q_token + qh * p.q_head + d, p.flip) : h8{};
+            const uint16_t* q = p.Q + t * p.q_token + qh * p.q_head;
+            Q[s] = d < D ? flip_query(load_query(q + d), p.flip) : h8{};
         }
         f16v O[DT];
 #pragma unroll

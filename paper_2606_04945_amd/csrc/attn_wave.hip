@@ -63,7 +63,7 @@ struct WaveRows {
 #pragma unroll
             for (int z = 0; z < 2 * P; ++z) {
                 const int d = 64 * (z / 2) + 16 * g + 8 * (z % 2);
-                Q[y][z] = d < p.D ? load_query(q + d, p.flip) : h8{};
+                Q[y][z] = d < p.D ? load_query(q + d) : h8{};
             }
             m[y] = kUnseen, l[y] = 0.0f;
 #pragma unroll
@@ -151,6 +151,10 @@ struct WaveRows {
             hold(p, q, 0, lane);
             keys(p, q, h, 0, c, g, r);
             values(p, q, h, 0, c, g, r);
+#pragma unroll
+            for (int y = 0; y < QT; ++y)
+#pragma unroll
+                for (int z = 0; z < 2 * P; ++z) Q[y][z] = flip_query(Q[y][z], p.flip);
             for (int j = 0; j + 1 < n; ++j) step<true>(p, q, h, j, lane, r);
             step<false>(p, q, h, n - 1, lane, r);
         }
@@ -269,6 +273,7 @@ template <int DP, int QT, int NW, bool WIDE>
 __global__ __launch_bounds__(NW* kWave) void attn_wave_kernel(AttnArgs p) {
     extern __shared__ __attribute__((aligned(16))) float lds[];
     constexpr int R = 16 * QT, LD = DP + 4;            // rows, padded row of floats
+    __builtin_assume(p.a.rows == R);
     float* ml = lds + NW * R * LD;                     // [wave][row] m, then l
     const int lane = threadIdx.x % kWave, c = lane % 16, g = lane / 16;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -280,14 +285,14 @@ __global__ __launch_bounds__(NW* kWave) void attn_wave_kernel(AttnArgs p) {
     const int worker = worker_of(p, all, wave, NW);
     if (!attn_always_direct(p.a) && blockIdx.x == 0 && threadIdx.x == 0) store_global(p.shared, (int)!all.direct);
     if (all.direct) {
-        const int64_t item = blockIdx.x / p.a.heads;
+        const int item = (int)blockIdx.x / p.a.heads;
         const Listed at = find_listed(p, item, first, lane);
         const int64_t r64 = item - list_start(at.q.s.t0, at.b, p.a.G, R, 1);
         if (r64 < 0 || r64 >= at.q.tiles) return;
         const AttnSteps steps = attn_steps(p.a, at.q.s, (int)r64);
         count = steps.count;
         stride = NW;
-        t = {at.q.s, at.b, (int)(blockIdx.x % p.a.heads), (int)r64,
+        t = {at.q.s, at.b, (int)blockIdx.x % p.a.heads, (int)r64,
              {0, steps.first + wave, steps.first + steps.count, false, false, false}};
     } else {
         if ((int)blockIdx.x >= p.a.groups) return;

@@ -138,6 +138,22 @@ extern "C" int plan(int T, int B, int Hq, int heads, int D, int max_len, int* o)
     return a.rows;
 }
 
+// 0 if the grid of tiles of 128 rows read tile by tile has every tile of every head once, and how far the XCDs'
+// numbers of places lie apart.
+extern "C" int spread(int T, int B, int heads, int G, int* apart) {
+    AttnShape a = attn_shape(T, B, heads * G, heads, 128, 1 << 20, true, 0);
+    a.rows = 128;
+    const int64_t grid = attn_grid(a), tiles = grid / heads;
+    if (grid % heads || tiles % attn_head_xcds(heads) || grid < attn_tile_slots(a)) return 1;
+    std::set<int64_t> seen;
+    for (int64_t at = 0; at < tiles; ++at) {
+        const int64_t t = attn_spread(at, tiles, attn_head_xcds(heads));
+        if (t < 0 || t >= tiles || !seen.insert(t).second) return 2;
+    }
+    *apart = (int)(grid % 8);
+    return 0;
+}
+
 // Whether a step of every sequence, `heads` key heads of G query heads, is read without splitting.
 extern "C" int direct(int B, int heads, int G, int max_len, int n, const int* lens) {
     const AttnShape a = attn_shape(B * n, B, heads * G, heads, 128, max_len, true, 0);
@@ -264,6 +280,16 @@ def test_which_kernel(plan):
     assert shape(8 * 32, 8, 32, 32, 64, 320) == (32, 256, 2048, 1)
     assert shape(8 * 2048, 8, 28, 4, 128, 2048) == (128, 512, 512, 0)
     assert shape(32, 1, 28, 4, 256, 64) == (128, 256, 256, 1)
+
+
+def test_tiles_go_round_the_xcds(plan):
+    for seed in range(60):
+        rng = random.Random(seed)
+        apart = ctypes.c_int(-1)
+        B = rng.randint(1, 40)
+        assert plan.spread(rng.randint(B, 5000), B, rng.choice([1, 2, 3, 4, 5, 6, 7, 8, 12, 16, 28, 32]),
+                           rng.randint(1, 16), ctypes.byref(apart)) == 0
+        assert apart.value == 0
 
 
 def test_direct_or_shared(plan):

@@ -100,6 +100,26 @@ def test_most_sequences():
                     torch.zeros(B + 1, 1, dtype=torch.int32, device="cuda"))
 
 
+def test_heads_that_do_not_divide_the_workgroups():
+    """Three key heads over a grid of a fixed number of workgroups, nearly all of them with a tile."""
+    page, heads, G, dim, n, B = 64, 3, 2, 16, 1490, 7
+    rng = np.random.default_rng(7)
+    pages = B * 24
+    cu, ln, table = ragged([n] * B, [n] * B, 24, page, pages, rng)
+    c = filled_cache(pages, heads, dim, page, rng)
+    q = normal(rng, n * B, heads * G, dim)
+    out = torch.full((n * B, heads * G, dim), 9.0, dtype=torch.float16, device="cuda")
+    sq.attn_kv8(dev(q), to_device(c), dev(cu), dev(ln), dev(table), causal=False, out=out)
+    rows = np.r_[0:3, 700:703, cu[1:] - 1, cu[1:-1], n * B - 130:n * B]
+    got = host(out)
+    assert not (got == 9).all(-1).any()
+    for b in range(B):
+        t = rows[(rows >= cu[b]) & (rows < cu[b + 1])]
+        one = np.array([0, len(t)], np.int32)
+        ref = A.attention(q[t], c, one, ln[b:b + 1], table[b:b + 1], causal=False)
+        check_attention(got[t], ref, b)
+
+
 @pytest.mark.parametrize("news", [[1, 1, 1], [20, 9, 1], [70, 100, 90]])
 def test_sequences_share_pages(news):
     """A common beginning in the same pages, several times the same page in one sequence; pages read back twice."""
