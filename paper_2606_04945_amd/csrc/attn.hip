@@ -14,8 +14,8 @@ namespace {
 // threads has a row, four channels a thread; where a workgroup has more groups than rows,
 // several share a row's results and meet in LDS in order.  Which worker ended first
 // changes nothing.  Bound by three round trips to memory that other XCDs wrote and, for
-// tiles of 128 rows, by the partial results' bytes (32 next tokens of 28 heads 9 us,
-// 2 x 512 tokens 15 us, 4 where nothing is shared).  Twice the workgroups: no change.
+// tiles of 128 rows, by the partial results' bytes (32 next tokens of 28 heads
+// 6.5 us, 2 x 512 tokens 15 us, 4 where nothing is shared).  Twice the workgroups: no change.
 constexpr int kJoinThreads = 256, kJoinGroups = 64;    // at most: heads of 16
 constexpr int kJoinBlocks = 512, kJoinMasks = kAttnCus * 8 / kWave;
 __global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(AttnArgs p) {

@@ -165,9 +165,9 @@ inline int64_t attn_tile_slots(const AttnShape& a) { return ((int64_t)a.T * a.G 
 // nothing joined (direct).  `total` is all tiles' weight, `most` the largest tile's.
 // Workgroups take tiles as they come free, so the last ends after about total / groups
 // if no tile is longer than that; splitting saves at most most - total / groups, and
-// costs the joining, as much as reading 1024 keys: one token over 518 keys 11.1 us
-// against 18.2 split, 2048 tokens of one sequence 77 against 110; 32 tokens of lengths
-// to 8192 58 us split.  (At 512 the first two split; 2048 changes no case measured.)
+// costs the joining, as much as reading 1024 keys: one token over 518 keys 10.4 us
+// against 17.5 split, 2048 tokens of one sequence 77 against 110; 32 tokens of lengths
+// to 8192 55 us split.  (At 512 the first two split; 2048 changes no case measured.)
 // Decided by every workgroup, from the lengths, and all come to the same answer.
 SQ_HD bool attn_always_direct(const AttnShape& a) { return a.max_len <= a.join; }   // all that the host can tell
 SQ_HD bool attn_direct(const AttnShape& a, int64_t total, int64_t most) {
@@ -212,7 +212,7 @@ inline int64_t attn_grid(const AttnShape& a) {
 
 // Waves of a workgroup that reads with single waves: what its registers hold without
 // spilling (tiles of 32 of heads to 128: eight instead of four, 8 blocks of 32 tokens
-// 38.5 -> 48.8 us).
+// 39.0 -> 48.8 us).
 inline int attn_waves(int rows, int D) { return rows * (D <= 64 ? 64 : D <= 128 ? 128 : 256) <= 16 * 128 ? 8 : 4; }
 
 inline AttnShape attn_shape(int T, int B, int Hq, int heads, int D, int max_len, bool causal, int window) {

@@ -47,9 +47,10 @@ struct Int {
 // scales; otherwise each block of 16 keys has its own.
 //
 // Bound by the matrix cores and by what shares their waves' issue slots: 8 prompts of up
-// to 2048 tokens (28 heads of 128 to 4) 402 us, 785 TFLOP/s, against 1127 of a large
-// library product.  Without the conversion of the codes 350 us, without the exponentials
-// 380, without the loads 375, without the maximum 397.  Tiles of 256 channels keep some
+// to 2048 tokens (28 heads of 128 to 4) 400 us, 790 TFLOP/s, against 1127 of a large
+// library product.  Of these the conversions of the codes cost 50, the loads 28, the
+// exponentials 22 and the maximum 5 (copies that leave them out).  A tile's begin and end
+// take as long as six of its steps: a sequence, its page, its codes, one after the other.  Tiles of 256 channels keep some
 // 240 registers in memory and are still ahead of tiles of 16 rows (199 us against 266
 // for 4 x 1024 tokens of 256 channels).
 template <int DP, bool WIDE>
