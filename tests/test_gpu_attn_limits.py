@@ -161,7 +161,24 @@ def test_queries_that_are_not_finite(news, lens):
     check_attention(dev(out), ref, news, dev(lse))
 
 
-@pytest.mark.parametrize("M", [1, 2, 17, 33, 65])
+def test_binding_refuses_workspaces_and_outputs():
+    rng = np.random.default_rng(8)
+    c = filled_cache(40, 2, 64, 64, rng)
+    cu, ln, table = ragged([1], [2000], 32, 64, 40, rng)
+    q = dev(normal(rng, 1, 8, 64))
+    args = (to_device(c), dev(cu), dev(ln), dev(table))
+    need = sq.attn_kv8_workspace_bytes(1, 1, 8, 2, 64, 32 * 64)
+    for kw, what in ((dict(ws=torch.empty(need, dtype=torch.uint8)), "ws"),
+                     (dict(ws=torch.empty(2 * need, dtype=torch.uint8, device="cuda")[::2]), "ws"),
+                     (dict(out=torch.empty(1, 8, 64, dtype=torch.float16)), "out"),
+                     (dict(lse=torch.empty(1, 7, dtype=torch.float32, device="cuda")), "lse")):
+        with pytest.raises(ValueError, match=what):
+            sq.attn_kv8(q, *args, **kw)
+    with pytest.raises(sq.StarQuantError, match="overlap"):
+        sq.attn_kv8(q, *args, out=q)
+
+
+@pytest.mark.parametrize("M", [1, 2, 17, 33, 65, 4099])
 @pytest.mark.parametrize("K,group", [(64, 32), (192, 64), (1088, 32)])
 def test_weight_only_rows_stay_apart(M, K, group):
     """K of half a step: what lies behind a row's end, a row of infinities or nothing, does not enter."""
