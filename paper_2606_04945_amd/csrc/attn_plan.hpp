@@ -190,8 +190,8 @@ constexpr int kAttnCus = 256;
 // Tiles of 128 rows read tile by tile: a head's tiles run on as few XCDs as share it,
 // which read the same keys, and go round them one by one, so that each has its share of
 // long sequences; the longest tiles of a sequence first.  Both together: 14 x 400 .. 862
-// tokens over 4000 keys 583 -> 536 us, over 1000 225 -> 212, 8 prompts of up to 2048 411
-// -> 400; either alone gains less than half of that.
+// tokens over 4000 keys 583 -> 536 us, over 1000 225 -> 212; either alone gains less, and
+// 8 prompts without older keys take the same time.
 SQ_HD int attn_head_xcds(int heads) {
     const int low = heads & -heads;                     // 8 XCDs
     return low >= 8 ? 1 : 8 / low;
