@@ -451,8 +451,9 @@ int kv_read(const sq_kv_cache* cache, const int32_t* list, int32_t n, uint16_t* 
  *   row that sees no key gives zeros, and lse -inf.
  *   Arithmetic: products of q with the codes summed in fp32 on the fp16 matrix
  *   cores, scales and softmax in fp32; the softmax weights times their value scale
- *   are rounded to fp16 (2^-11 relative) for the second product, summed in fp32, and
- *   the result is rounded once to fp16.
+ *   are rounded to fp16 for the second product (2^-11 relative, or 2^-36 of the row's
+ *   largest such product where that is more), summed in fp32, and the result is
+ *   rounded once to fp16.
  *   Q    [T][Hq][dim] fp16, strides as in sq_rope.   O out [T][Hq][dim] fp16, dense,
  *        overlapping neither Q nor the cache.
  *   lse  out [T][Hq] fp32, the natural logarithm of the softmax's sum, or NULL.

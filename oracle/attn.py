@@ -170,17 +170,18 @@ def attention(q, cache, cu, lens, table, causal=True, window=0, scale=None):
     return out, lse, dict(spread=spread, vmax=vmax, total=total, terms=terms, mass=mass)
 
 
-def attention_bounds(out, lse, e, D):
+def attention_bounds(out, lse, e, D, floor=2.0 ** -36):
     """How far fp32 sums and logits, fp16 weights and one fp16 rounding may be from fp64.
 
     A logit sums D products in fp32 (each addition 2^-24 of the sum of magnitudes) and is scaled twice and
-    subtracted from the maximum (3 roundings); 2^x of fp32 adds 2^-22 relative.  A weight times its value scale is
-    rounded to fp16: half a step, 2^-11 relative or 2^-25 of the largest value scale below fp16's normal range, for
-    codes up to 128; the softmax's sum is at least its largest term, 1.  Both sums over the terms are in fp32."""
+    subtracted from the reference (3 roundings); 2^x of fp32 adds 2^-22 relative.  A weight times its value scale is
+    rounded to fp16: half a step, 2^-11 relative or, below fp16's normal range, 2^-25 where the row's largest is at
+    2^11 or more: `floor` of the largest value scale, for codes up to 128; the softmax's sum is at least its largest
+    term, 1.  Both sums over the terms are in fp32."""
     logit = (D + 6) * 2.0 ** -24 * e["mass"] + 2.0 ** -21
     rel = 2.0 ** -11 + 2 * logit + e["terms"] * 2.0 ** -23 + 2.0 ** -20
     b_out = (2.0 ** -11 * np.abs(out) + 2.0 ** -25 + rel[..., None] * e["spread"]
-             + (e["terms"] * 2.0 ** -25 * 128 * e["vmax"] / e["total"])[..., None])
+             + (e["terms"] * floor * 128 * e["vmax"] / e["total"])[..., None])
     b_lse = logit + e["terms"] * 2.0 ** -24 + 2.0 ** -20 + 4 * 2.0 ** -24 * np.abs(np.where(np.isfinite(lse), lse, 0))
     return b_out, b_lse
 

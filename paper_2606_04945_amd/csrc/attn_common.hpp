@@ -5,10 +5,14 @@
 // are, every int8 being an fp16; a page's key scale multiplies its logits in fp32.
 // Its value scale s goes into the weight: with x the logit times log2 e,
 //   w = 2^(x + log2 s - m),  O = sum w code,  l = sum w / s,  out = O / l,
-// and m a running reference close to the largest x + log2 s, so that a weight is
-// rounded to fp16 relative to the row's largest contribution however the scales
-// differ, and the rounding of log2 s cancels between O and l.  Where the reference
-// rises to m', O and l are multiplied by 2^(m - m').
+// and m a running reference below the largest x + log2 s, so that a weight is rounded
+// to fp16 relative to the row's largest contribution however the scales differ, and
+// the rounding of log2 s cancels between O and l.  Where the reference rises to m', O
+// and l are multiplied by 2^(m - m').  How far below: fp16 holds weights from 2^-14 on
+// with 11 bits, smaller ones with half a step of 2^-25, and a row whose largest weight
+// meets small values consists of its small weights.  So the largest is near the upper
+// end, at 2^14 in tiles of 16 and 32 rows, between 2^11 and 2^15 in those of 128, whose
+// reference may lag: half a step is 2^-39 and 2^-36 of it.
 //
 // Both products are formed transposed, S^T = K Q^T and O^T = V^T P^T: a lane then
 // has one query's logits, which are where the second product wants that query's
@@ -265,14 +269,14 @@ constexpr float kHidden = -3e38f, kUnseen = -1e12f;
 
 // What a block of 16 keys (one page) multiplies: logits by ks, and w by 2^lv with
 // 1 / s = iv.  Keys of no page, or past the length, take no part: lv = -inf.  A value
-// scale below 2^-100, 0 included, counts as that: its contribution to an fp16 result
-// is 0 either way.  The limits also keep infinite and NaN scales of hidden keys from
-// spoiling a weight of 0.
+// scale below 2^-60, 0 included, counts as that: its contribution to an fp16 result
+// is 0 either way, and 2^28 weights of 2^15 times 2^60 have a sum in fp32.  The limits
+// also keep infinite and NaN scales of hidden keys from spoiling a weight of 0.
 struct BlockScale {
     float ks, lv, iv;
 };
 __device__ __forceinline__ BlockScale block_scale(bool in, float ks, float vs, float scale) {
-    const float s = fminf(fmaxf(vs, 0x1p-100f), 3e38f);
+    const float s = fminf(fmaxf(vs, 0x1p-60f), 3e38f);
     const float k = fminf(fmaxf(ks * scale, 1e-25f), 3e38f);
     return {in ? k : 0.0f, in ? __builtin_amdgcn_logf(s) : kNone, in ? 1.0f / s : 0.0f};
 }

@@ -7,6 +7,8 @@ namespace {
 
 typedef float f16v __attribute__((ext_vector_type(16)));
 
+constexpr float kLargest = 11.0f, kMost = 15.0f;    // log2 of a row's largest weight: set to, and let grow to
+
 // LDS of the tile kernel: two buffers of a step's keys [64][DP], two of its values
 // [DP][64], as halves.  16-byte chunks of a row are swapped by the row so that 16
 // lanes reading one chunk of 16 rows take 16 different bank groups.
@@ -251,10 +253,10 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_tile_kernel(AttnA
                 mx = fmaxf(mx, __builtin_fmaf(bm, k.ks, k.lv));
             }
             mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
-            // the reference may lag behind by 8: weights to 2^8 keep their precision, and the
+            // the reference follows once the largest weight would pass 2^15, so that the
             // accumulators are rescaled a few times a row
-            if (__any(mx > m + 8.0f)) {
-                const float mn = fmaxf(m, mx), fade = __builtin_amdgcn_exp2f(m - mn);
+            if (__any(mx > m + kMost)) {
+                const float mn = fmaxf(m, mx - kLargest), fade = __builtin_amdgcn_exp2f(m - mn);
                 m = mn;
                 l *= fade;
 #pragma unroll

@@ -17,6 +17,8 @@
 namespace sq {
 namespace {
 
+constexpr float kLargest = 14.0f;     // log2 of a row's largest weight
+
 // over the four 16-lane groups of a wave
 __device__ __forceinline__ float groups_max(float x) {
     x = fmaxf(x, __shfl_xor(x, 16, kWave));
@@ -202,7 +204,7 @@ struct WaveRows {
             for (int e = 0; e < 4; ++e)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) mx = fmaxf(mx, S[y][e][i]);
-            mx = fmaxf(m[y], groups_max(__builtin_fmaf(mx, bs.ks, bs.lv)));
+            mx = fmaxf(m[y], groups_max(__builtin_fmaf(mx, bs.ks, bs.lv)) - kLargest);
             const float fade = __builtin_amdgcn_exp2f(m[y] - mx), off = bs.lv - mx;
             m[y] = mx;
             float sum = 0.0f;
