@@ -262,10 +262,15 @@ __device__ __forceinline__ h8 to_halves(uint32_t w0, uint32_t w1) {
     return r;
 }
 
-// A hidden key's product and the reference of a row that has seen no key.  A hidden
-// key's logit is below -1e13 for any key scale (those count as 1e-25 at least), far
-// below the reference, so its weight is 0 without a test; no real logit comes near.
-constexpr float kHidden = -3e38f, kUnseen = -1e12f;
+// A hidden key's product, and the reference of a row that has seen no key: as low as a
+// logit can be, and finite, so that a hidden key's weight is 0 without a test.
+constexpr float kHidden = -__builtin_inff(), kUnseen = -0x1.fffffep127f;
+
+// Logits of larger magnitude are rounded before the reference is subtracted from them, which
+// takes an instruction more for each: the usual form subtracts it from the product itself,
+// and where fp32 rounds logits by more than a bit or two the largest, which the reference was
+// taken from, may be that much above it.  A reference there is the largest itself.
+constexpr float kFine = 0x1p18f;
 
 // What a block of 16 keys (one page) multiplies: logits by ks, and w by 2^lv with
 // 1 / s = iv.  Keys of no page, or past the length, take no part: lv = -inf.  A value
@@ -278,7 +283,7 @@ struct BlockScale {
 __device__ __forceinline__ BlockScale block_scale(bool in, float ks, float vs, float scale) {
     const float s = fminf(fmaxf(vs, 0x1p-60f), 3e38f);
     const float k = fminf(fmaxf(ks * scale, 1e-25f), 3e38f);
-    return {in ? k : 0.0f, in ? __builtin_amdgcn_logf(s) : kNone, in ? 1.0f / s : 0.0f};
+    return {in ? k : 1.0f, in ? __builtin_amdgcn_logf(s) : kNone, in ? 1.0f / s : 0.0f};
 }
 
 __device__ __forceinline__ h8 load_query(const uint16_t* q) {

@@ -243,7 +243,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_tile_kernel(AttnA
                     for (int e = 0; e < 16; ++e)
                         if ((uint32_t)(32 * y + 8 * (e / 4) + e % 4) - from >= span) S[y][e] = kHidden;
             }
-            float mx = kUnseen;
+            float mx = kNone;
 #pragma unroll
             for (int z = 0; z < 4; z += 4 / Z) {
                 float bm = S[z / 2][8 * (z % 2)];
@@ -253,10 +253,19 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_tile_kernel(AttnA
                 mx = fmaxf(mx, __builtin_fmaf(bm, k.ks, k.lv));
             }
             mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
+            if (__any(fabsf(mx) > kFine)) {
+#pragma unroll
+                for (int e = 0; e < 32; ++e) {
+                    const BlockScale& k = bs[e / 8 * Z / 4];
+                    S[e / 16][e % 16] = __builtin_fmaf(S[e / 16][e % 16], k.ks, k.lv);
+                }
+#pragma unroll
+                for (int z = 0; z < Z; ++z) bs[z].ks = 1.0f, bs[z].lv = 0.0f;
+            }
             // the reference follows once the largest weight would pass 2^15, so that the
             // accumulators are rescaled a few times a row
-            if (__any(mx > m + kMost)) {
-                const float mn = fmaxf(m, mx - kLargest), fade = __builtin_amdgcn_exp2f(m - mn);
+            if (__any(mx - m > kMost)) {
+                const float mn = fmaxf(m, fabsf(mx) > kFine ? mx : mx - kLargest), fade = __builtin_amdgcn_exp2f(m - mn);
                 m = mn;
                 l *= fade;
 #pragma unroll

@@ -204,16 +204,26 @@ struct WaveRows {
             for (int e = 0; e < 4; ++e)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) mx = fmaxf(mx, S[y][e][i]);
-            mx = fmaxf(m[y], groups_max(__builtin_fmaf(mx, bs.ks, bs.lv)) - kLargest);
-            const float fade = __builtin_amdgcn_exp2f(m[y] - mx), off = bs.lv - mx;
+            mx = groups_max(__builtin_fmaf(mx, bs.ks, bs.lv));
+            float ks = bs.ks, lv = bs.lv, largest = kLargest;
+            if (__any(fabsf(mx) > kFine)) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) S[y][e][i] = __builtin_fmaf(S[y][e][i], ks, lv);
+                ks = 1.0f, lv = 0.0f;
+                if (fabsf(mx) > kFine) largest = 0.0f;
+            }
+            mx = fmaxf(m[y], mx - largest);
+            const float fade = __builtin_amdgcn_exp2f(m[y] - mx), off = lv - mx;
             m[y] = mx;
             float sum = 0.0f;
 #pragma unroll
             for (int e = 0; e < 4; ++e)
 #pragma unroll
                 for (int i = 0; i < 4; i += 2) {
-                    const f2 w = {__builtin_amdgcn_exp2f(__builtin_fmaf(S[y][e][i], bs.ks, off)),
-                                  __builtin_amdgcn_exp2f(__builtin_fmaf(S[y][e][i + 1], bs.ks, off))};
+                    const f2 w = {__builtin_amdgcn_exp2f(__builtin_fmaf(S[y][e][i], ks, off)),
+                                  __builtin_amdgcn_exp2f(__builtin_fmaf(S[y][e][i + 1], ks, off))};
                     sum += w[0];
                     sum += w[1];
                     const h2 x = __builtin_convertvector(w, h2);
