@@ -460,7 +460,8 @@ int kv_read(const sq_kv_cache* cache, const int32_t* list, int32_t n, uint16_t* 
  *   ws   device workspace of at least sq_attn_kv8_workspace_bytes() for the same
  *        sizes, max_len = max_pages page.  Its contents need no preparation; two
  *        calls that may run at the same time need one each.
- *   A NaN or an infinity in a query spoils that query's row alone.
+ *   A row is NaN, and its lse, if its query holds a NaN or an infinity, or if it sees a
+ *   key of a page whose scale is a NaN, an infinity or negative; no other row is.
  *   T Hq / 16 + B heads < 2^23; T Hq (Hq / heads) B (max_pages page + 64) < 2^63.
  */
 size_t sq_attn_kv8_workspace_bytes(int32_t T, int32_t B, int32_t Hq, int32_t heads, int32_t dim, int32_t max_len);

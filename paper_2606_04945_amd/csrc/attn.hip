@@ -105,7 +105,7 @@ __global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(AttnArgs p) {
             if (!in || gi % per || m == kNone) continue;      // no maximum: one worker wrote the row
             const int at = t.row0 + row;
             const int64_t o = (int64_t)(t.t0 + at / G) * p.a.heads * G + t.h * G + at % G;
-            store_result(p.O + o * D + 4 * v, O, l > 0.0f ? 1.0f / l : 0.0f);
+            store_result(p.O + o * D + 4 * v, O, inverse(m, l));
             if (p.lse && v == 0) store_global(p.lse + o, result_lse(m, l));
         }
     }

@@ -262,9 +262,11 @@ __device__ __forceinline__ h8 to_halves(uint32_t w0, uint32_t w1) {
     return r;
 }
 
-// A hidden key's product, and the reference of a row that has seen no key: as low as a
-// logit can be, and finite, so that a hidden key's weight is 0 without a test.
-constexpr float kHidden = -__builtin_inff(), kUnseen = -0x1.fffffep127f;
+// A hidden key's product, and the reference of a row that has seen no key: low, and
+// finite, so that a hidden key's weight is 0 without a test.  A page whose scales are not
+// finite numbers >= 0 has the logit kBad, which no others come near: a row that sees a key
+// of it ends with that reference, and is NaN.
+constexpr float kHidden = -__builtin_inff(), kUnseen = -0x1p126f, kBad = 0x1p120f;
 
 // Logits of larger magnitude are rounded before the reference is subtracted from them, which
 // takes an instruction more for each: the usual form subtracts it from the product itself,
@@ -276,14 +278,15 @@ constexpr float kFine = 0x1p18f;
 // 1 / s = iv.  Keys of no page, or past the length, take no part: lv = -inf.  A value
 // scale below 2^-60, 0 included, counts as that: its contribution to an fp16 result
 // is 0 either way, and 2^28 weights of 2^15 times 2^60 have a sum in fp32.  The limits
-// also keep infinite and NaN scales of hidden keys from spoiling a weight of 0.
+// of the key scale keep its products finite, and above 0, so that a hidden key's stay -inf.
 struct BlockScale {
     float ks, lv, iv;
 };
 __device__ __forceinline__ BlockScale block_scale(bool in, float ks, float vs, float scale) {
-    const float s = fminf(fmaxf(vs, 0x1p-60f), 3e38f);
-    const float k = fminf(fmaxf(ks * scale, 1e-25f), 3e38f);
-    return {in ? k : 1.0f, in ? __builtin_amdgcn_logf(s) : kNone, in ? 1.0f / s : 0.0f};
+    constexpr int kNot = 0x001 | 0x002 | 0x004 | 0x008 | 0x010 | 0x200;     // classes: NaN, -inf, negative, inf
+    const bool bad = __builtin_amdgcn_classf(ks, kNot) | __builtin_amdgcn_classf(vs, kNot);
+    const float s = fminf(fmaxf(vs, 0x1p-60f), 0x1p100f), lv = bad ? kBad : __builtin_amdgcn_logf(s);
+    return {in & !bad ? fminf(fmaxf(ks * scale, 1e-25f), 3e38f) : 1.0f, in ? lv : kNone, __builtin_amdgcn_rcpf(s)};
 }
 
 __device__ __forceinline__ h8 load_query(const uint16_t* q) {
@@ -294,6 +297,20 @@ __device__ __forceinline__ h8 flip_query(h8 q, uint32_t flip) {
     return __builtin_bit_cast(h8, __builtin_bit_cast(v4i, q) ^ (int)flip);
 }
 
+// NaN if a query is not finite, else 0
+template <int N>
+__device__ __forceinline__ float query_fault(const h8 (&q)[N]) {
+    h8 z{};
+#pragma unroll
+    for (int i = 0; i < N; ++i) z += q[i] * (_Float16)0.0f;
+    return (float)(((z[0] + z[1]) + (z[2] + z[3])) + ((z[4] + z[5]) + (z[6] + z[7])));
+}
+
+// what a row's sums are multiplied by at the end: 0 of a row that has seen no key
+__device__ __forceinline__ float inverse(float m, float l) {
+    return l == 0.0f ? 0.0f : m < kBad / 2 ? 1.0f / l : __builtin_nanf("");
+}
+
 // four results of a row as fp16
 __device__ __forceinline__ void store_result(uint16_t* o, f4 x, float inv) {
     const u32x2 w = {(uint32_t)f2h(x[0] * inv) | ((uint32_t)f2h(x[1] * inv) << 16),
@@ -302,7 +319,7 @@ __device__ __forceinline__ void store_result(uint16_t* o, f4 x, float inv) {
 }
 
 __device__ __forceinline__ float result_lse(float m, float l) {
-    return l == 0.0f ? kNone : (m + __builtin_amdgcn_logf(l)) * kLn2;      // NaN of a NaN
+    return l == 0.0f ? kNone : m < kBad / 2 ? (m + __builtin_amdgcn_logf(l)) * kLn2 : __builtin_nanf("");
 }
 
 }  // namespace

@@ -333,10 +333,22 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_tile_kernel(AttnA
             }
         }
         l += __shfl_xor(l, 32, kWave);
+        const bool none = s0 < s1 && l == 0.0f && lo < hi;
+        if (__any(none)) {                             // products of -inf, where a query is infinite
+            h8 q[KS];
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                const int d = 16 * s + 8 * half;
+                q[s] = d < D ? load_query(p.Q + t * p.q_token + qh * p.q_head + d) : h8{};
+            }
+            float fault = query_fault(q);
+            fault += __shfl_xor(fault, 32, kWave);
+            if (none) l = fault;
+        }
         if (row < rows) {
             const int64_t o = (int64_t)t * p.a.heads * G + qh;
             const int lr = wave * 32 + c;
-            const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+            const float inv = inverse(m, l);
             const bool split = part.begins_inside || part.ends_inside, any = s0 < s1 && !part.whole;
             float* ws = p.places + attn_place(worker, part.begins_inside) * attn_place_floats(R, D);
 #pragma unroll

@@ -161,7 +161,15 @@ struct WaveRows {
             step<false>(p, q, h, n - 1, lane, r);
         }
 #pragma unroll
-        for (int y = 0; y < QT; ++y) l[y] = groups_sum(l[y]);
+        for (int y = 0; y < QT; ++y) {
+            l[y] = groups_sum(l[y]);
+            // no weight at all: products of -inf, where a query is infinite
+            const bool none = first < end && l[y] == 0.0f && lo[y] < hi[y];
+            if (__any(none)) {
+                const float fault = groups_sum(query_fault(Q[y]));
+                if (none) l[y] = fault;
+            }
+        }
     }
 
     template <bool MORE>
@@ -250,7 +258,7 @@ struct WaveRows {
 #pragma unroll
         for (int y = 0; y < QT; ++y) {
             if (!in[y]) continue;
-            const float inv = l[y] > 0.0f ? 1.0f / l[y] : 0.0f;
+            const float inv = inverse(m[y], l[y]);
             const int64_t o = (int64_t)t[y] * p.a.heads * p.a.G + qh[y];
 #pragma unroll
             for (int d = 0; d < DT; ++d)
@@ -353,7 +361,7 @@ __global__ __launch_bounds__(NW* kWave) void attn_wave_kernel(AttnArgs p) {
             }
             const int at = t.r * R + row;
             const int64_t o = (int64_t)(t.s.t0 + at / p.a.G) * p.a.heads * p.a.G + t.h * p.a.G + at % p.a.G;
-            store_result(p.O + o * p.D + d, O, l > 0.0f ? 1.0f / l : 0.0f);
+            store_result(p.O + o * p.D + d, O, inverse(m, l));
             if (p.lse && d == 0) store_global(p.lse + o, result_lse(m, l));
         }
         return;
