@@ -423,8 +423,9 @@ int sq_rope(const uint16_t* X, int64_t x_token, int64_t x_head, const int32_t* p
  *   Qr may be Q with the same strides.
  *   pos  [T] int32 rotary positions; NULL: the cache positions.
  *   (T / page + 2 B) heads + T Hq dim / 4096 < 2^24 (/ 512 if rot % 16 != 0).
- *   Keys and values are finite; what a NaN or an infinity becomes is not defined,
- *   in its page and head, and nowhere else.
+ *   A NaN or an infinity among a page's new (rotated) keys of a head, or its values,
+ *   makes that scale NaN and the new codes zero; so it stays until slot 0 is written
+ *   again, and what reads the page gets NaN (attn_kv8: in rows that see a key of it).
  * kv_read: the listed pages as values code scale, rounded to fp16: K and V
  *   [n][heads][page][dim]; zeros for an entry that is no page.  n heads < 2^24.
  */

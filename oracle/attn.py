@@ -65,11 +65,13 @@ class Cache:
 
 
 def _quantised(x, old, fresh):
-    """fp32 scale and codes of x [tokens, D] against a page's scale `old`."""
+    """fp32 scale and codes of x [tokens, D] against a page's scale `old`; NaN and zero codes if one is not finite."""
     s = np.float32(np.abs(x).max(initial=0.0).astype(np.float32) / np.float32(127))
     if not fresh:
-        s = max(np.float32(old), s)
-    if s == 0:
+        s = np.maximum(np.float32(old), s)             # NaN if one is
+    if not np.isfinite(s):
+        s = np.float32(np.nan)
+    if not s > 0:
         return s, np.zeros(x.shape, np.int8)
     q = np.rint((x.astype(np.float32) / s).astype(np.float32))
     return s, np.clip(q, -128, 127).astype(np.int8)

@@ -158,21 +158,33 @@ struct Span {
     int64_t ph;
 };
 
+// The larger of two values, NaN if one is: a page must not lose what went wrong upstream.
+__device__ __forceinline__ float largest(float x, float y) { return __builtin_elementwise_maximum(x, y); }
+
 // largest over the workgroup of two values at once
 __device__ __forceinline__ void block_max(float& x, float& y, float* red) {
-    x = wave_max(x);
-    y = wave_max(y);
+#pragma unroll
+    for (int o = kWave / 2; o > 0; o >>= 1) {
+        x = largest(x, __shfl_xor(x, o, kWave));
+        y = largest(y, __shfl_xor(y, o, kWave));
+    }
     if (threadIdx.x % kWave == 0) red[threadIdx.x / kWave] = x, red[kThreads / kWave + threadIdx.x / kWave] = y;
     __syncthreads();
     x = red[0], y = red[kThreads / kWave];
 #pragma unroll
     for (int w = 1; w < kThreads / kWave; ++w) {
-        x = fmaxf(x, red[w]);
-        y = fmaxf(y, red[kThreads / kWave + w]);
+        x = largest(x, red[w]);
+        y = largest(y, red[kThreads / kWave + w]);
     }
 }
 
-// codes of 8 values against scale s, y = 1 / s, a byte each; zero codes for s = 0
+// A page's scale from its old one and the new magnitudes' largest: NaN if not finite.
+__device__ __forceinline__ float page_scale(float old, float most) {
+    const float s = largest(old, most / 127.0f);
+    return s < __builtin_inff() ? s : __builtin_nanf("");
+}
+
+// codes of 8 values against scale s, y = 1 / s, a byte each; zero codes for s = 0 or NaN
 __device__ __forceinline__ void codes8(const float* x, float s, float y, uint32_t& lo, uint32_t& hi) {
     int c[8];
     quant_codes8<127>(x, s, y, c);
@@ -285,7 +297,7 @@ __device__ void append_registers(const AppendArgs& a, const Span& p, int h, uint
 #pragma unroll
         for (int z = 0; z < 8; ++z) {
             x[u][z] = xa[z], x[u][8 + z] = xb[z];
-            km = fmaxf(km, fmaxf(fabsf(xa[z]), fabsf(xb[z])));
+            km = largest(km, largest(fabsf(xa[z]), fabsf(xb[z])));
         }
     }
 #pragma unroll
@@ -294,10 +306,10 @@ __device__ void append_registers(const AppendArgs& a, const Span& p, int h, uint
         for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int q = 0; q < 4; ++q)
-                vm = fmaxf(vm, fmaxf(fabsf(h2f((uint16_t)(uint32_t)vv[u][j][q])),
-                                     fabsf(h2f((uint16_t)((uint32_t)vv[u][j][q] >> 16)))));
+                vm = largest(vm, largest(fabsf(h2f((uint16_t)(uint32_t)vv[u][j][q])),
+                                         fabsf(h2f((uint16_t)((uint32_t)vv[u][j][q] >> 16)))));
     block_max(km, vm, red);
-    const float ks = fmaxf(ks0, km / 127.0f), ky = 1.0f / ks, vs = fmaxf(vs0, vm / 127.0f), vy = 1.0f / vs;
+    const float ks = page_scale(ks0, km), ky = 1.0f / ks, vs = page_scale(vs0, vm), vy = 1.0f / vs;
     if (tid == 0) a.k_scale[p.ph] = ks, a.v_scale[p.ph] = vs;
     int8_t *kc = a.k + p.ph * a.page * D, *vc = a.v + p.ph * a.page * D;
     if (p.s0 && ks > ks0) rescale_keys(kc, p.s0 * D, ks0 / ks);
@@ -355,14 +367,14 @@ __device__ void append_pairs(const AppendArgs& a, const Span& p, int h, float* l
             rope_angle(a.pos ? a.pos[p.row + i] : p.pos + i, a.freq[r.pair], a.amp, false, c[0], s[0]);
             rope_turn<1>(u, v, c, s, a.layout);
         }
-        km = fmaxf(km, fmaxf(fabsf(u[0]), fabsf(v[0])));
+        km = largest(km, largest(fabsf(u[0]), fabsf(v[0])));
         lds[i * D + r.a] = u[0];
         lds[i * D + r.b] = v[0];
     }
     for (int e = tid; e < n * D; e += kThreads)
-        vm = fmaxf(vm, fabsf(h2f(a.V[(p.row + e / D) * a.v_token + h * a.v_head + e % D])));
+        vm = largest(vm, fabsf(h2f(a.V[(p.row + e / D) * a.v_token + h * a.v_head + e % D])));
     block_max(km, vm, red);
-    const float ks = fmaxf(ks0, km / 127.0f), ky = 1.0f / ks, vs = fmaxf(vs0, vm / 127.0f), vy = 1.0f / vs;
+    const float ks = page_scale(ks0, km), ky = 1.0f / ks, vs = page_scale(vs0, vm), vy = 1.0f / vs;
     if (tid == 0) a.k_scale[p.ph] = ks, a.v_scale[p.ph] = vs;
     int8_t *kc = a.k + p.ph * a.page * D, *vc = a.v + p.ph * a.page * D;
     if (p.s0 && ks > ks0) rescale_keys(kc, p.s0 * D, ks0 / ks);
