@@ -476,7 +476,8 @@ int attn_kv8(const uint16_t* Q, int64_t q_token, int64_t q_head, const sq_kv_cac
  * for each output channel and group of `group` inputs, for linears whose
  * activations stay unquantised at decode.
  *   sq_quantize_weights_group: per group s = fp16(absmax / 7), codes
- *     clamp(rint(w / s), -8, 7) against the rounded s (zero codes for s = 0).
+ *     clamp(rint(w / s), -8, 7) against the rounded s (zero codes for s = 0).  A group that
+ *     holds a NaN or an infinity has that for its scale and zero codes: its products are NaN.
  *     W [N][K] fp16 in; Wq [N][K/2] packed int4 out, s_w [K / group][N] fp16 out.
  *   w4a16_gemm_frag: Y[m][n] = fp16(sum_G s_w[G][n] sum_{k in G} X[m][k] q[n][k]),
  *     sums in fp32, each group's scale applied to its fp32 sum.  X [M][K] fp16, Wf

@@ -197,7 +197,7 @@ def quantize_group(W, group):
     s = (np.abs(x).max(-1) / np.float32(7)).astype(np.float32).astype(np.float16)
     sf = s.astype(np.float32)[..., None]
     with np.errstate(divide="ignore", invalid="ignore"):
-        q = np.where(sf > 0, np.clip(np.rint(x / sf), -8, 7), 0)
+        q = np.where((sf > 0) & np.isfinite(sf), np.clip(np.rint(x / sf), -8, 7), 0)
     return q.reshape(N, K).astype(np.int64), np.ascontiguousarray(s.T)
 
 

@@ -225,14 +225,17 @@ __global__ __launch_bounds__(256) void quantize_group_kernel(const uint16_t* __r
     if (item >= (int64_t)N * ng) return;
     const int n = (int)(item / ng), gi = (int)(item % ng);
     const uint32_t* w = reinterpret_cast<const uint32_t*>(W + (int64_t)n * K + gi * group);
-    float m = 0.0f;
-    for (int e = lane; e < group / 2; e += kWave) m = fmaxf(m, fmaxf(fabsf(lo_h(w[e])), fabsf(hi_h(w[e]))));
-    m = wave_max(m);
+    float m = 0.0f;                                    // NaN if a weight is
+    for (int e = lane; e < group / 2; e += kWave)
+        m = __builtin_elementwise_maximum(m, __builtin_elementwise_maximum(fabsf(lo_h(w[e])), fabsf(hi_h(w[e]))));
+#pragma unroll
+    for (int o = kWave / 2; o > 0; o >>= 1) m = __builtin_elementwise_maximum(m, __shfl_xor(m, o, kWave));
     const uint16_t sh = f2h(m / 7.0f);
     const float s = h2f(sh);
+    const bool some = s > 0.0f && s < __builtin_inff();
     uint8_t* q = Wq + ((int64_t)n * K + gi * group) / 2;
     for (int e = lane; e < group / 2; e += kWave) {
-        const int a = s > 0.0f ? quant4(lo_h(w[e]), s) : 0, b = s > 0.0f ? quant4(hi_h(w[e]), s) : 0;
+        const int a = some ? quant4(lo_h(w[e]), s) : 0, b = some ? quant4(hi_h(w[e]), s) : 0;
         q[e] = (uint8_t)((a & 15) | ((b & 15) << 4));
     }
     if (lane == 0) s_w[(int64_t)gi * N + n] = sh;
