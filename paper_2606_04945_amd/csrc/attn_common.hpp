@@ -136,8 +136,7 @@ __device__ __forceinline__ Survey survey(const AttnArgs& p, const Group& first, 
     for (int b0 = 0;;) {
         const AttnSeq q = group_seq(p, g);
         total += lane_value(wave_scan(q.weight), kWave - 1);
-        const int64_t last = q.tiles > 0 ? q.base + q.slope * (q.tiles - 1) : 0;
-        most = max(most, wave_max64(last));
+        most = max(most, wave_max64(attn_most(q)));
         b0 += kWave;
         if (b0 >= p.a.B) break;
         g = load_group(p, b0, lane);

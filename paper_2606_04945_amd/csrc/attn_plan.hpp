@@ -12,7 +12,8 @@
 // a partial result, and a second kernel joins them.
 //
 // Weights only balance the load: tile r of a sequence weighs base + slope r, a
-// closed form that needs no loop over tiles.
+// closed form that needs no loop over tiles: its keys and a step's, within a factor of
+// two of them with a window.
 #pragma once
 #include "kv_plan.hpp"
 
@@ -49,6 +50,11 @@ SQ_HD AttnSeq attn_seq(const AttnShape& a, int c0, int c1, int len) {
     if (a.causal && !a.window) {
         q.slope = a.rows;
         q.base = (int64_t)a.G * ((q.s.off > 0 ? q.s.off : 0) + kAttnStep) + a.rows;
+    } else if (a.window && !a.causal) {
+        // a query sees all later keys: the window's length and the tokens from its own on, but no
+        // more than there are, which a line leaves out
+        q.slope = -a.rows;
+        q.base = a.G * ((int64_t)q.s.n + (a.window < q.s.len ? a.window : q.s.len) + kAttnStep);
     } else {
         const int64_t reach = (int64_t)a.window + a.rows / a.G + 1;
         const int64_t span = a.window && reach < q.s.len ? reach : q.s.len;
@@ -57,6 +63,10 @@ SQ_HD AttnSeq attn_seq(const AttnShape& a, int c0, int c1, int len) {
     }
     q.weight = q.tiles * q.base + q.slope * ((int64_t)q.tiles * (q.tiles - 1) / 2);
     return q;
+}
+// Weight of the largest tile.
+SQ_HD int64_t attn_most(const AttnSeq& q) {
+    return q.tiles > 0 ? q.base + (q.slope > 0 ? q.slope * (q.tiles - 1) : 0) : 0;
 }
 
 // Weight of the tiles before tile r of one key head.

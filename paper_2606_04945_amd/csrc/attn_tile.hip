@@ -79,7 +79,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_tile_kernel(AttnA
         const Listed l = find_listed(p, item, first, lane);
         const int64_t r64 = item - list_start(l.q.s.t0, l.b, G, R, 1);
         if (r64 < 0 || r64 >= l.q.tiles) return;
-        const int r = l.q.tiles - 1 - (int)r64;
+        const int r = l.q.slope < 0 ? (int)r64 : l.q.tiles - 1 - (int)r64;       // the longest first
         const AttnSteps steps = attn_steps(p.a, l.q.s, r);
         tile = {l.q.s, l.b, (int)(at / tiles), r,
                 {0, steps.first, steps.first + steps.count, true, false, false}};
