@@ -459,7 +459,8 @@ int kv_read(const sq_kv_cache* cache, const int32_t* list, int32_t n, uint16_t* 
  *        overlapping neither Q nor the cache.
  *   lse  out [T][Hq] fp32, the natural logarithm of the softmax's sum, or NULL.
  *   ws   device workspace of at least sq_attn_kv8_workspace_bytes() for the same
- *        sizes, max_len = max_pages page.  Its contents need no preparation; two
+ *        sizes, max_len = max_pages page.  One for T tokens, B sequences and a max_len
+ *        is enough for fewer of each.  Its contents need no preparation; two
  *        calls that may run at the same time need one each.
  *   A row is NaN, and its lse, if its query holds a NaN or an infinity, or if it sees a
  *   key of a page whose scale is a NaN, an infinity or negative; no other row is.

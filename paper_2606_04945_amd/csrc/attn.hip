@@ -114,8 +114,7 @@ __global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(AttnArgs p) {
 }  // namespace
 
 size_t attn_workspace_bytes(int T, int B, int Hq, int heads, int D, int max_len) {
-    const AttnShape a = attn_shape(T, B, Hq, heads, D, max_len, true, 0);
-    return attn_always_direct(a) ? 0 : (size_t)attn_workspace(a, D);
+    return (size_t)attn_workspace_most(T, B, Hq, heads, D, max_len);
 }
 
 hipError_t launch_attn(const uint16_t* Q, int64_t q_token, int64_t q_head, const int8_t* k, const int8_t* v,

@@ -225,14 +225,32 @@ inline int64_t attn_grid(const AttnShape& a) {
 // 39.0 -> 48.8 us).
 inline int attn_waves(int rows, int D) { return rows * (D <= 64 ? 64 : D <= 128 ? 128 : 256) <= 16 * 128 ? 8 : 4; }
 
-inline AttnShape attn_shape(int T, int B, int Hq, int heads, int D, int max_len, bool causal, int window) {
-    const int G = Hq / heads;
-    const int64_t rows = (int64_t)T * G;
-    AttnShape a{T, B, heads, G, max_len, causal, window, 0, kAttnCus, 0, 1024};
-    a.rows = rows > (int64_t)64 * B ? 128 : rows > (int64_t)16 * B && D <= 128 ? 32 : 16;
-    if (a.rows == 128) a.groups = a.workers = D <= 128 ? 2 * kAttnCus : kAttnCus;
-    else a.workers = a.groups * attn_waves(a.rows, D);
+inline AttnShape attn_shape_of_rows(int rows, int T, int B, int Hq, int heads, int D, int max_len, bool causal,
+                                    int window) {
+    AttnShape a{T, B, heads, Hq / heads, max_len, causal, window, rows, kAttnCus, 0, 1024};
+    if (rows == 128) a.groups = a.workers = D <= 128 ? 2 * kAttnCus : kAttnCus;
+    else a.workers = a.groups * attn_waves(rows, D);
     return a;
+}
+inline AttnShape attn_shape(int T, int B, int Hq, int heads, int D, int max_len, bool causal, int window) {
+    const int64_t rows = (int64_t)T * (Hq / heads);
+    return attn_shape_of_rows(rows > (int64_t)64 * B ? 128 : rows > (int64_t)16 * B && D <= 128 ? 32 : 16, T, B, Hq,
+                              heads, D, max_len, causal, window);
+}
+
+// The most that a batch of up to T tokens and B sequences needs: of every tile that one of
+// them can take, so that a workspace made for the largest batch serves the others.
+inline int64_t attn_workspace_most(int T, int B, int Hq, int heads, int D, int max_len) {
+    const int64_t rows = (int64_t)T * (Hq / heads);
+    int64_t most = 0;
+    for (int r : {16, 32, 128}) {
+        if ((r == 32 && (rows <= 16 || D > 128)) || (r == 128 && rows <= 64)) continue;
+        const AttnShape a = attn_shape_of_rows(r, T, B, Hq, heads, D, max_len, true, 0);
+        if (attn_always_direct(a)) return 0;
+        const int64_t n = attn_workspace(a, D);
+        most = n > most ? n : most;
+    }
+    return most;
 }
 
 }  // namespace sq
