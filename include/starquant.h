@@ -355,7 +355,8 @@ int tac_calibrate(const uint16_t* Z_fp, const uint16_t* Z_q, int32_t N, int32_t 
  *      allowed.
  *   pos  [T] int32 positions, any sign; NULL: the token's index.
  *   freq [rot / 2] fp64, radians per position: sq_rope_frequencies or one's own.
- *   D % 16 == 0, 16 <= D <= 1024; rot even, 2 <= rot <= D; T H D < 2^33.
+ *   D % 16 == 0, 16 <= D <= 1024; rot even, 2 <= rot <= D; T H D < 2^33, at most
+ *   2^33 - 512 if rot % 16 != 0.
  *
  * sq_rope_frequencies fills freq with base^(-2 j / rot), scaled for contexts
  * `factor` >= 1 times the original:
@@ -422,7 +423,8 @@ int sq_rope(const uint16_t* X, int64_t x_token, int64_t x_head, const int32_t* p
  *   K, V [T][heads][dim] and Q, Qr [T][Hq][dim] fp16 with strides as in sq_rope;
  *   Qr may be Q with the same strides.
  *   pos  [T] int32 rotary positions; NULL: the cache positions.
- *   (T / page + 2 B) heads + T Hq dim / 4096 < 2^24 (/ 512 if rot % 16 != 0).
+ *   (T / page + 2 B) heads + T Hq dim / 4096, rounded up, < 2^24 (/ 512 if rot % 16
+ *   != 0).
  *   A NaN or an infinity among a page's new (rotated) keys of a head, or its values,
  *   makes that scale NaN and the new codes zero; so it stays until slot 0 is written
  *   again, and what reads the page gets NaN (attn_kv8: in rows that see a key of it).

@@ -622,8 +622,9 @@ int sq_rope(const uint16_t* X, int64_t x_token, int64_t x_head, const int32_t* p
     SQ_REQUIRE(D >= 16 && D <= 1024 && D % 16 == 0, SQ_ERR_SHAPE, "sq_rope: D=%d: need a multiple of 16 in 16 .. 1024",
                D);
     SQ_TRY(check_rotation(rot, layout, amplitude, D, "sq_rope"));
-    SQ_REQUIRE(T >= 0 && H >= 0 && (double)T * H * D < 0x1p33, SQ_ERR_SHAPE, "sq_rope: T=%d H=%d: need T H D < 2^33", T,
-               H);
+    // (a pair a thread where rot % 16 != 0, and the last workgroup's threads are all there)
+    SQ_REQUIRE(T >= 0 && H >= 0 && (double)T * H * D < (rot % 16 ? 0x1p33 - 511 : 0x1p33), SQ_ERR_SHAPE,
+               "sq_rope: T=%d H=%d: need T H D < 2^33, at most 2^33 - 512 for rot %% 16 != 0", T, H);
     if (T == 0 || H == 0) return SQ_OK;
     SQ_TRY(check_strides(x_token, x_head, T, H, D, false, "sq_rope", "X"));
     SQ_TRY(check_strides(y_token, y_head, T, H, D, true, "sq_rope", "Y"));
@@ -649,7 +650,8 @@ int kv_append(const sq_kv_cache* cache, const uint16_t* K, int64_t k_token, int6
     SQ_REQUIRE(!Q || (freq && Qr), SQ_ERR_NULL, "kv_append: Q needs freq and Qr");
     SQ_REQUIRE(!Q || (Hq >= 1 && Hq <= 1024), SQ_ERR_SHAPE, "kv_append: Hq=%d: need 1 .. 1024", Hq);
     const int64_t per = freq && rot % 16 ? 512 : 4096;       // entries of Q that a workgroup rotates, at least
-    SQ_REQUIRE(((int64_t)T / c.page + 2 * (int64_t)B) * c.heads + (Q ? (int64_t)T * Hq * c.dim / per : 0) < kMaxBlocks,
+    SQ_REQUIRE(((int64_t)T / c.page + 2 * (int64_t)B) * c.heads + (Q ? ((int64_t)T * Hq * c.dim + per - 1) / per : 0) <
+                   kMaxBlocks,
                SQ_ERR_SHAPE, "kv_append: T=%d B=%d: too many rows for one call", T, B);
     if (T == 0 || B == 0) return SQ_OK;
     SQ_TRY(check_strides(k_token, k_head, T, c.heads, c.dim, false, "kv_append", "K"));
