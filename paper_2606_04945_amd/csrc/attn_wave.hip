@@ -195,7 +195,7 @@ struct WaveRows {
             if (((j + 1) * q.per & (kWave - 1)) == 0) hold(p, q, j + 1, lane);
             keys(p, q, h, j + 1, c, g, r);
         }
-        h8 W[QT][2];
+        float top[QT], most = 0.0f, ks = bs.ks, lv = bs.lv;
 #pragma unroll
         for (int y = 0; y < QT; ++y) {
             if (!__all(key0 >= lo[y] && key0 + kAttnStep <= hi[y])) {
@@ -212,17 +212,30 @@ struct WaveRows {
             for (int e = 0; e < 4; ++e)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) mx = fmaxf(mx, S[y][e][i]);
-            mx = groups_max(__builtin_fmaf(mx, bs.ks, bs.lv));
-            float ks = bs.ks, lv = bs.lv, largest = kLargest;
-            if (__any(fabsf(mx) > kFine)) {
+            mx = groups_max(__builtin_fmaf(mx, ks, lv));
+            top[y] = mx - kLargest;
+            most = fmaxf(most, fabsf(mx));
+        }
+        if (__any(most > kFine)) {
+#pragma unroll
+            for (int y = 0; y < QT; ++y) {
+                float mx = kNone;
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) S[y][e][i] = __builtin_fmaf(S[y][e][i], ks, lv);
-                ks = 1.0f, lv = 0.0f;
-                if (fabsf(mx) > kFine) largest = 0.0f;
+                    for (int i = 0; i < 4; ++i) {
+                        S[y][e][i] = __builtin_fmaf(S[y][e][i], ks, lv);
+                        mx = fmaxf(mx, S[y][e][i]);
+                    }
+                mx = groups_max(mx);
+                if (fabsf(mx) > kFine) top[y] = mx;
             }
-            mx = fmaxf(m[y], mx - largest);
+            ks = 1.0f, lv = 0.0f;
+        }
+        h8 W[QT][2];
+#pragma unroll
+        for (int y = 0; y < QT; ++y) {
+            const float mx = fmaxf(m[y], top[y]);
             const float fade = __builtin_amdgcn_exp2f(m[y] - mx), off = lv - mx;
             m[y] = mx;
             float sum = 0.0f;
