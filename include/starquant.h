@@ -367,7 +367,8 @@ int tac_calibrate(const uint16_t* Z_fp, const uint16_t* Z_q, int32_t N, int32_t 
  *   SQ_ROPE_YARN    a pair that makes beta_fast turns or more over the original
  *                   context (`original` tokens) as it is, one that makes beta_slow
  *                   or fewer divided by factor, linear in the turns between (the
- *                   YaRN paper's 32 and 1); beta_fast > beta_slow >= 0.
+ *                   YaRN paper's 32 and 1); beta_fast > beta_slow >= 0.  (A model whose
+ *                   ramp is linear in the pair's index needs frequencies of its own.)
  * sq_rope_amplitude: what YaRN scales cos and sin by, 0.1 ln(factor) + 1; 1 for
  * the others.
  */
@@ -464,8 +465,10 @@ int kv_read(const sq_kv_cache* cache, const int32_t* list, int32_t n, uint16_t* 
  *        sizes, max_len = max_pages page.  One for T tokens, B sequences and a max_len
  *        is enough for fewer of each.  Its contents need no preparation; two
  *        calls that may run at the same time need one each.
- *   A row is NaN, and its lse, if its query holds a NaN or an infinity, or if it sees a
- *   key of a page whose scale is a NaN, an infinity or negative; no other row is.
+ *   A row is NaN, and its lse, if it sees a key and its query holds a NaN or an infinity,
+ *   or if it sees a key of a page whose scale is a NaN, an infinity or negative; no other
+ *   row is (but one of such a query may be where it sees none).  Logits are below 2^118 in
+ *   magnitude.
  *   T Hq / 16 + B heads < 2^23; T Hq (Hq / heads) B (max_pages page + 64) < 2^63.
  */
 size_t sq_attn_kv8_workspace_bytes(int32_t T, int32_t B, int32_t Hq, int32_t heads, int32_t dim, int32_t max_len);

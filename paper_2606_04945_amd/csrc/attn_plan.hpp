@@ -175,9 +175,11 @@ inline int64_t attn_tile_slots(const AttnShape& a) { return ((int64_t)a.T * a.G 
 // nothing joined (direct).  `total` is all tiles' weight, `most` the largest tile's.
 // Workgroups take tiles as they come free, so the last ends after about total / groups
 // if no tile is longer than that; splitting saves at most most - total / groups, and
-// costs the joining, as much as reading 1024 keys: one token over 518 keys 10.4 us
+// costs the joining, as much as reading 1024 keys: one token over 518 keys 10.6 us
 // against 17.5 split, 2048 tokens of one sequence 77 against 110; 32 tokens of lengths
-// to 8192 55 us split.  (At 512 the first two split; 2048 changes no case measured.)
+// to 8192 55 us split.  (At 512 the first two split.  At 2048 tiles of 128 rows gain where
+// there are about as many as workgroups, 3000 tokens of one sequence 165 -> 99 us, and lose
+// for heads above 128, 1500 tokens 143 -> 236.)
 // Decided by every workgroup, from the lengths, and all come to the same answer.
 SQ_HD bool attn_always_direct(const AttnShape& a) { return a.max_len <= a.join; }   // all that the host can tell
 SQ_HD bool attn_direct(const AttnShape& a, int64_t total, int64_t most) {
@@ -194,7 +196,9 @@ SQ_HD bool attn_direct(const AttnShape& a, int64_t total, int64_t most) {
 // 16 / 32 / 128, 8 sequences of 32 heads of 128, 2000 older keys and another 12 tokens
 // 28.4 / 33.2 / -, 24: 42.8 / 35.8 / 57.8, 56: 72.8 / 60.2 / 63.5, 96: - / 89.3 / 76.2,
 // 128: - / 111.5 / 80.1.  Heads of 256 take 16 rows at a time, or 128 where there are
-// more than 64 (4 x 1024 tokens 266 / - / 199).
+// more than 64 (4 x 1024 tokens 266 / - / 206).  A call has one size, by its average: 512
+// tokens among 63 next tokens over caches of 2000 keys (32 heads to 32) take tiles of 16,
+// 294 us, the two apart 63 and 217; with 8 key heads tiles of 32, 134 us, apart 64 and 55.
 constexpr int kAttnCus = 256;
 
 // Tiles of 128 rows read tile by tile: a head's tiles run on as few XCDs as share it,

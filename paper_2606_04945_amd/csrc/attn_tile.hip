@@ -49,12 +49,14 @@ struct Int {
 // scales; otherwise each block of 16 keys has its own.
 //
 // Bound by the matrix cores and by what shares their waves' issue slots: 8 prompts of up
-// to 2048 tokens (28 heads of 128 to 4) 400 us, 790 TFLOP/s, against 1127 of a large
-// library product.  Of these the conversions of the codes cost 50, the loads 28, the
-// exponentials 22 and the maximum 5 (copies that leave them out).  A tile's begin and end
-// take as long as six of its steps: a sequence, its page, its codes, one after the other.  Tiles of 256 channels keep some
-// 240 registers in memory and are still ahead of tiles of 16 rows (199 us against 266
-// for 4 x 1024 tokens of 256 channels).
+// to 2048 tokens (28 heads of 128 to 4) 400 to 430 us with the card's clock, 740 to 790
+// TFLOP/s, against 1127 of a large library product.  In a series at 400 us the conversions
+// of the codes cost 50, the loads 28, the exponentials 22 and the maximum 5 (copies that
+// leave them out).  A tile's begin and end take as long as six of its steps: a sequence, its
+// page, its codes, one after the other.  All 256 registers are in use: tiles of 128 channels
+// keep 39 more in memory (56 for small pages), outside the loop over keys; those of 256 some
+// 320, with about 30 loads a step in the loop, and are still ahead of tiles of 16 rows (206 us
+// against 266 for 4 x 1024 tokens of 256 channels).
 template <int DP, bool WIDE>
 __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_tile_kernel(AttnArgs p) {
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];

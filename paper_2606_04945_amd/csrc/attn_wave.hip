@@ -10,8 +10,9 @@
 // Bound by reading the codes where there are many of them (2 x 131072 keys of 8 heads of
 // 128: 97 us, 4.9 TB/s; 32 next tokens over 6000 keys on average 38 us, 5.2 TB/s, the
 // joining apart); by the round trips of a step where there are few (one token of 32
-// heads over 518 keys: 10.4 us); by the longest tile's steps where a batch is read tile by
-// tile (8 blocks of 32 tokens of 32 heads over up to 2080 keys: 34 us, 3.3 TB/s).
+// heads over 518 keys: 10.6 us in a series of calls); by the longest tile's steps where a
+// batch is read tile by tile (8 blocks of 32 tokens of 32 heads over up to 2080 keys: 36 us,
+// 3.1 TB/s).
 #include "attn_common.hpp"
 
 namespace sq {
