@@ -417,10 +417,10 @@ int sq_rope(const uint16_t* X, int64_t x_token, int64_t x_head, const int32_t* p
  *   A page whose slot 0 is written takes its scale from the new tokens; another
  *   keeps max(its scale, theirs), and where that grows its older codes become
  *   rint(code s_old / s_new).  Calling it again with the same arguments changes
- *   nothing (except that queries rotated in place turn again).  Codes of slots from the length on keep their bytes.  New tokens
- *   before position 0 (a length shorter than their number) are dropped.  No two
- *   table entries that a call writes through may name the same page (several
- *   sequences may read one).
+ *   nothing (except that queries rotated in place turn again).  Codes of slots from
+ *   the length on keep their bytes.  New tokens before position 0 (a length shorter
+ *   than their number) are dropped.  No two table entries that a call writes through
+ *   may name the same page (several sequences may read one).
  *   K, V [T][heads][dim] and Q, Qr [T][Hq][dim] fp16 with strides as in sq_rope;
  *   Qr may be Q with the same strides.
  *   pos  [T] int32 rotary positions; NULL: the cache positions.

@@ -267,7 +267,8 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_tile_kernel(AttnA
             // the reference follows once the largest weight would pass 2^15, so that the
             // accumulators are rescaled a few times a row
             if (__any(mx - m > kMost)) {
-                const float mn = fmaxf(m, fabsf(mx) > kFine ? mx : mx - kLargest), fade = __builtin_amdgcn_exp2f(m - mn);
+                const float mn = fmaxf(m, fabsf(mx) > kFine ? mx : mx - kLargest);
+                const float fade = __builtin_amdgcn_exp2f(m - mn);
                 m = mn;
                 l *= fade;
 #pragma unroll
