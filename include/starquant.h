@@ -496,6 +496,95 @@ int sq_quantize_weights_group(const uint16_t* W, int32_t N, int32_t K, int32_t g
 int w4a16_gemm_frag(const uint16_t* X, const uint8_t* Wf, const uint16_t* s_w, int32_t M, int32_t N, int32_t K,
                     int32_t group, uint16_t* Y, void* stream);
 
+/*
+ * Products with a fused epilogue: what follows a quantised product in a layer, applied to
+ * its sums before they are stored.
+ *   t = (float(acc) s_a[m]) s_w[n] + bias[n]     (w4a16_linear: the fp32 sum of
+ *                                                 w4a16_gemm_frag in place of the first term)
+ *   y = act(t)                                    [M][N], or, gated,
+ *   y[m][f] = act(t[m][f]) t[m][N / 2 + f]        [M][N / 2]
+ *   Y = y + residual, rounded to Y's type; all in fp32.
+ * Without activation and gate Y differs from a separate addition only in the rounding that
+ * is left out.
+ *   act      SQ_ACT_NONE; RELU max(t, 0); RELU2 its square; SILU t / (1 + e^-t); GELU
+ *            t Phi(t); GELU_TANH t / (1 + e^(-2 sqrt(2 / pi) (t + 0.044715 t^3))).
+ *   glu      non-zero: gated.  The N weight rows are the N / 2 gates and then their ups;
+ *            N % 16 == 0.  Wf is then from sq_weights_to_frag_glu (_w8), which stores
+ *            group g of 16 rows as gates 8 g .. 8 g + 7 followed by their ups, in the
+ *            fragment order of sq_weights_to_frag; s_w and bias keep the rows' order.
+ *   bias     [N] fp16, or NULL.
+ *   residual [M][N or N / 2] of Y's type, or NULL; it may be Y itself.
+ *   f32      non-zero: Y and residual are fp32, else fp16.
+ *   Y        dense; apart from `residual` it overlaps no input.
+ * The other arguments, rules and workspace are those of w4a4_gemm_frag, w8a8_gemm_frag
+ * (sq_gemm_workspace_bytes, sq_gemm_w8_workspace_bytes for the same M, N, K) and
+ * w4a16_gemm_frag (which needs none; s_w [K / group][N]).  A NULL epilogue is one of zeros.
+ */
+#define SQ_ACT_NONE 0
+#define SQ_ACT_RELU 1
+#define SQ_ACT_RELU2 2
+#define SQ_ACT_SILU 3
+#define SQ_ACT_GELU 4
+#define SQ_ACT_GELU_TANH 5
+typedef struct sq_epilogue {
+    const uint16_t* bias;
+    const void* residual;
+    int32_t act, glu, f32;
+} sq_epilogue;
+int sq_weights_to_frag_glu(const uint8_t* Wq, int32_t N, int32_t K, uint8_t* Wf, void* stream);
+int sq_weights_to_frag_glu_w8(const int8_t* Wq, int32_t N, int32_t K, uint8_t* Wf, void* stream);
+int w4a4_linear(const uint8_t* Aq, const float* s_a, const uint8_t* Wf, const float* s_w, int32_t M, int32_t N,
+                int32_t K, const sq_epilogue* epilogue, void* Y, void* ws, size_t ws_bytes, void* stream);
+int w8a8_linear(const int8_t* Aq, const float* s_a, const uint8_t* Wf, const float* s_w, int32_t M, int32_t N,
+                int32_t K, const sq_epilogue* epilogue, void* Y, void* ws, size_t ws_bytes, void* stream);
+int w4a16_linear(const uint16_t* X, const uint8_t* Wf, const uint16_t* s_w, int32_t M, int32_t N, int32_t K,
+                 int32_t group, const sq_epilogue* epilogue, void* Y, void* stream);
+
+/*
+ * sq_norm -- the norm ahead of a block, with the residual stream that the block before it
+ * adds to, and the quantiser of the product behind it:
+ *   u  = y,  or with y_weight  ((y - mean(y)) r(y)) y_weight   (the norm after a block)
+ *   u  = u gate[seq];   h' = h + u alpha, rounded to h's type;  h' = h without y
+ *   n  = ((h' - mean(h')) r(h')) weight;   n = n (1 + scale[seq]);   n = n + shift[seq]
+ *   X  = fp16(n);   codes, s = the quantiser of sgat_quantize on the rows G_state n
+ * r(x) = 1 / sqrt(mean((x - mean(x))^2) + eps); without `center` the means count as 0 (RMS
+ * norm).  Sums are in fp64, mean and r rounded once to fp32; every other step is one fp32
+ * operation in the order written.  What is NULL is left out.
+ *   h        [M][K] fp16, or fp32 if `f32`.        y  [M][K] fp16, the block's output.
+ *   gate, scale, shift  [seqs][K] fp16 each, their rows gate_row ... elements apart (multiples
+ *            of 8, at least K; of no account for one row): per-sequence conditioning, or
+ *            with one row a layer's own scales and biases.
+ *   seq      [M] int32 (4-byte aligned), the row of those that a token takes, clamped to 0 ..
+ *            seqs - 1; NULL: row 0.
+ *   y_weight, weight  [K] fp16.                    alpha, eps  finite, eps > 0.
+ *   h_out    [M][K] of h's type; may be h.  X [M][K] fp16.
+ *   codes, s [M][K / 2] packed int4 (bits = 4) or [M][K] int8 (bits = 8) and [M] fp32, both
+ *            or neither; state, d_m, d_u as in sgat_quant_act.  A row that holds (or makes) a NaN
+ *            or an infinity has scale NaN and zero codes.
+ *   At least one of h_out, X and codes.  Outputs overlap nothing else.
+ *   K % 8 == 0, 8 <= K <= 32768; with codes K % 64 == 0.  Any M >= 0.
+ */
+typedef struct sq_norm_args {
+    const void* h;
+    const uint16_t* y;
+    const uint16_t* y_weight;
+    const uint16_t* gate;
+    const uint16_t* scale;
+    const uint16_t* shift;
+    int64_t gate_row, scale_row, shift_row;
+    const int32_t* seq;
+    const uint16_t* weight;
+    const uint8_t* state;
+    void* h_out;
+    uint16_t* X;
+    void* codes;
+    float* s;
+    double eps;
+    float alpha;
+    int32_t seqs, f32, center, bits, d_m, d_u;
+} sq_norm_args;
+int sq_norm(const sq_norm_args* args, int32_t M, int32_t K, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

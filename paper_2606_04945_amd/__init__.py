@@ -16,6 +16,12 @@ Between the projections, attention over a paged 8-bit cache:
     freq = rope_frequencies(dim, 1e6)
     q = kv_append(cache, k, v, cu, lens, table, freq=freq, q=q)
     Z = attn_kv8(q, cache, cu, lens, table)
+
+Between the products, the residual stream, norms and activations:
+
+    Aq, s_a, h = norm_quant(h, y, weight=w, state=state)
+    y = w4a4_linear(Aq, s_a, Wf, s_w, act="silu", glu=True)
+    h = w4a4_linear(*sgat_quant_act(y, state), Wf2, s_w2, residual=h)
 """
 from __future__ import annotations
 
@@ -25,7 +31,7 @@ from typing import NamedTuple, Optional, Tuple
 
 import torch
 
-from ._lib import KVCacheStruct, SQ_OK, StarQuantError, check, lib  # noqa: F401
+from ._lib import EpilogueStruct, KVCacheStruct, NormStruct, SQ_OK, StarQuantError, check, lib  # noqa: F401
 
 __all__ = ["sgat_prepare_weights", "sgat_transform", "sgat_quantize", "sgat_quant_act", "w4a4_gemm", "tac_apply",
            "tac_default_block", "default_band", "quant_act_workspace_bytes", "gemm_workspace_bytes",
@@ -35,7 +41,8 @@ __all__ = ["sgat_prepare_weights", "sgat_transform", "sgat_quantize", "sgat_quan
            "fp6_row_bytes", "codes_to_fp6", "w4a4_gemm_fp6",
            "frag_weight_bytes", "weights_to_frag", "w4a4_gemm_frag", "w8a8_gemm_frag",
            "rope_frequencies", "rope_amplitude", "rope", "KVCache", "kv_cache", "kv_append", "kv_read", "attn_kv8",
-           "attn_kv8_workspace_bytes", "quantize_weights_group", "w4a16_gemm_frag"]
+           "attn_kv8_workspace_bytes", "quantize_weights_group", "w4a16_gemm_frag",
+           "w4a4_linear", "w8a8_linear", "w4a16_linear", "norm", "norm_quant"]
 
 
 def _on_stream(fn):
@@ -315,10 +322,11 @@ def _frag_shape(N: int, K: int, bits: int):
 
 
 @_on_stream
-def weights_to_frag(Wq: torch.Tensor, *, out=None, stream=None):
+def weights_to_frag(Wq: torch.Tensor, *, glu: bool = False, out=None, stream=None):
     """Code matrix -> fragment order [k steps, ceil(N/16), 1024] (uint8): packed
     int4 weights [N, K/2] (uint8, 128 codes a k step) or int8 weights [N, K]
-    (int8, 64 codes a k step)."""
+    (int8, 64 codes a k step).  glu=True: rows are N/2 gates and then their ups,
+    stored in alternating blocks of 8 for the gated *_linear calls."""
     N, Kc = Wq.shape
     bits = 8 if Wq.dtype == torch.int8 else 4
     K = Kc if bits == 8 else 2 * Kc
@@ -328,7 +336,10 @@ def weights_to_frag(Wq: torch.Tensor, *, out=None, stream=None):
     if out is None:
         out = torch.empty(shape, dtype=torch.uint8, device=Wq.device)
     _need(out, "out", torch.uint8, shape)
-    f = lib().sq_weights_to_frag_w8 if bits == 8 else lib().sq_weights_to_frag
+    if glu:
+        f = lib().sq_weights_to_frag_glu_w8 if bits == 8 else lib().sq_weights_to_frag_glu
+    else:
+        f = lib().sq_weights_to_frag_w8 if bits == 8 else lib().sq_weights_to_frag
     check(f(_ptr(Wq), N, K, _ptr(out), _stream(stream)))
     return out
 
@@ -689,3 +700,155 @@ def w4a16_gemm_frag(X: torch.Tensor, Wf: torch.Tensor, s_w: torch.Tensor, *, Y=N
         _need(Y, "Y", torch.float16, (M, N))
     _run(lib().w4a16_gemm_frag, (X, Wf, s_w, Y), (_ptr(X), _ptr(Wf), _ptr(s_w), M, N, K, K // ng, _ptr(Y)), stream)
     return Y
+
+
+ACTIVATIONS = {"none": 0, "relu": 1, "relu2": 2, "silu": 3, "gelu": 4, "gelu_tanh": 5}
+_FLOATS = (torch.float16, torch.float32)
+
+
+def _epilogue(M: int, N: int, like: torch.Tensor, bias, act: str, glu: bool, residual, Y, dtype):
+    """Checks what a fused epilogue takes; returns it and Y."""
+    if glu and N % 16:
+        raise ValueError(f"glu needs N % 16 == 0, got N={N}")
+    shape = (M, N // 2 if glu else N)
+    if dtype is None:
+        dtype = Y.dtype if Y is not None else residual.dtype if residual is not None else torch.float16
+    if dtype not in _FLOATS:
+        raise ValueError(f"the output must be torch.float16 or torch.float32, got {dtype}")
+    _need(bias, "bias", torch.float16, (N,), optional=True)
+    _need(residual, "residual", dtype, shape, optional=True)
+    if Y is None:
+        Y = torch.empty(shape, dtype=dtype, device=like.device)
+    else:
+        _need(Y, "Y", dtype, shape)
+    return EpilogueStruct(_ptr(bias), _ptr(residual), _choice(ACTIVATIONS, act, "act"), int(glu),
+                          int(dtype is torch.float32)), Y
+
+
+@_on_stream
+def w4a4_linear(Aq: torch.Tensor, s_a: torch.Tensor, Wf: torch.Tensor, s_w: torch.Tensor, *, bias=None,
+                act: str = "none", glu: bool = False, residual=None, Y=None, dtype: Optional[torch.dtype] = None, ws=None,
+                stream=None, bits: int = 4):
+    """w4a4_gemm_frag with bias [N] fp16, activation ("none", "relu", "relu2", "silu", "gelu" or
+    "gelu_tanh") and residual in its epilogue: Y = act(t) + residual with t the dequantised
+    product plus bias.  glu=True: the rows of W are N/2 gates and then their ups
+    (weights_to_frag(glu=True); s_w and bias in the rows' order), Y = act(t_gate) t_up + residual
+    [M, N/2].  Y and residual are both fp16 or both fp32 (dtype; default the residual's, else fp16);
+    Y may be the residual.  bits=8 takes int8 codes."""
+    M, Kc = Aq.shape
+    N = s_w.shape[0]
+    K = Kc if bits == 8 else 2 * Kc
+    _need(Aq, "Aq", torch.int8 if bits == 8 else torch.uint8)
+    _need(Wf, "Wf", torch.uint8, _frag_shape(N, K, bits))
+    _need(s_a, "s_a", torch.float32, (M,))
+    _need(s_w, "s_w", torch.float32, (N,))
+    e, Y = _epilogue(M, N, Aq, bias, act, glu, residual, Y, dtype)
+    ws, wsb = _ws(gemm_workspace_bytes(M, N, K, bits), ws, Aq.device)
+    _run(lib().w8a8_linear if bits == 8 else lib().w4a4_linear, (Aq, s_a, Wf, s_w, bias, residual, Y, ws),
+         (_ptr(Aq), _ptr(s_a), _ptr(Wf), _ptr(s_w), M, N, K, e, _ptr(Y), _ptr(ws), wsb), stream)
+    return Y
+
+
+def w8a8_linear(Aq, s_a, Wf, s_w, **kw):
+    return w4a4_linear(Aq, s_a, Wf, s_w, bits=8, **kw)
+
+
+@_on_stream
+def w4a16_linear(X: torch.Tensor, Wf: torch.Tensor, s_w: torch.Tensor, *, bias=None, act: str = "none",
+                 glu: bool = False, residual=None, Y=None, dtype: Optional[torch.dtype] = None, stream=None):
+    """w4a16_gemm_frag (fp16 rows X [M, K], 4-bit weights, scales s_w [K/group, N]) with the epilogue
+    of w4a4_linear.  Made for few rows."""
+    M, K = X.shape
+    ng, N = s_w.shape
+    if ng < 1 or K % ng:
+        raise ValueError(f"s_w has {ng} groups, which do not divide K={K}")
+    _need(X, "X", torch.float16)
+    _need(Wf, "Wf", torch.uint8, _frag_shape(N, K, 4))
+    _need(s_w, "s_w", torch.float16, (ng, N))
+    e, Y = _epilogue(M, N, X, bias, act, glu, residual, Y, dtype)
+    _run(lib().w4a16_linear, (X, Wf, s_w, bias, residual, Y),
+         (_ptr(X), _ptr(Wf), _ptr(s_w), M, N, K, K // ng, e, _ptr(Y)), stream)
+    return Y
+
+
+def _norm(h, y, weight, post_weight, gate, alpha, scale, shift, seq, eps, center, h_out, X, codes, s, state, d_m, d_u,
+          bits, stream):
+    """One sq_norm call on checked outputs; returns h_out (h itself without y)."""
+    M, K = h.shape
+    dt = h.dtype
+    if dt not in _FLOATS:
+        raise ValueError(f"h must be torch.float16 or torch.float32, got {dt}")
+    _need(h, "h", dt)
+    _need(y, "y", torch.float16, (M, K), optional=True)
+    _need(weight, "weight", torch.float16, (K,), optional=True)
+    _need(post_weight, "post_weight", torch.float16, (K,), optional=True)
+    _need(state, "state", torch.uint8, (M,), optional=True)
+    _need(seq, "seq", torch.int32, (M,), optional=True)
+    if y is None and (post_weight is not None or gate is not None):
+        raise ValueError("post_weight and gate need y")
+    seqs, strides = None, []
+    for t, name in ((gate, "gate"), (scale, "scale"), (shift, "shift")):
+        if t is None:
+            strides.append(0)
+            continue
+        n = t.shape[0] if t.dim() == 2 else 1
+        if not t.is_cuda or t.dtype is not torch.float16 or t.dim() not in (1, 2) or t.shape[-1] != K:
+            raise ValueError(f"{name} must be a torch.float16 device tensor of shape [K={K}] or [seqs, K]")
+        if t.stride(-1) != 1:
+            raise ValueError(f"{name} must be dense in its last dimension")
+        if n == 0 or (seqs is not None and n != seqs):
+            raise ValueError("gate, scale and shift must have the same number of rows, at least one")
+        seqs = n
+        strides.append(t.stride(0) if t.dim() == 2 else K)
+    if seqs is not None and seqs > 1 and seq is None and M > 0:
+        raise ValueError("seq is required where gate, scale and shift have several rows")
+    if h_out is not None:
+        _need(h_out, "h_out", dt, (M, K))
+    elif y is not None:
+        h_out = torch.empty_like(h)
+    a = NormStruct(_ptr(h), _ptr(y), _ptr(post_weight), _ptr(gate), _ptr(scale), _ptr(shift), *strides, _ptr(seq),
+                   _ptr(weight), _ptr(state), _ptr(h_out), _ptr(X), _ptr(codes), _ptr(s), eps, alpha, seqs or 0,
+                   int(dt is torch.float32), int(center), bits, d_m, d_u)
+    _run(lib().sq_norm, (h, y, weight, post_weight, gate, scale, shift, seq, state, h_out, X, codes, s), (a, M, K), stream)
+    return h if h_out is None else h_out
+
+
+@_on_stream
+def norm(h: torch.Tensor, y: Optional[torch.Tensor] = None, *, weight=None, post_weight=None, gate=None,
+         alpha: float = 1.0, scale=None, shift=None, seq=None, eps: float = 1e-6, center: bool = False, out=None,
+         h_out=None, stream=None):
+    """The block output y [M, K] onto the residual stream h [M, K] (fp16 or fp32), and the norm of
+    the sum: h' = h + alpha gate y (y normed itself with post_weight), X = norm(h') weight (1 + scale)
+    + shift, fp16.  RMS norm, or with center=True the mean taken off.  gate, scale and shift are
+    [seqs, K] fp16 (rows any multiple of 8 apart) of which token i takes row seq[i], or [K].  Without y
+    h' is h.  Returns (X, h'); h_out may be h."""
+    M, K = h.shape
+    if out is None:
+        out = torch.empty((M, K), dtype=torch.float16, device=h.device)
+    _need(out, "out", torch.float16, (M, K))
+    h_out = _norm(h, y, weight, post_weight, gate, alpha, scale, shift, seq, eps, center, h_out, out, None, None, None,
+                  0, 0, 0, stream)
+    return out, h_out
+
+
+@_on_stream
+def norm_quant(h: torch.Tensor, y: Optional[torch.Tensor] = None, *, state=None, d_m: Optional[int] = None,
+               d_u: Optional[int] = None, weight=None, post_weight=None, gate=None, alpha: float = 1.0, scale=None,
+               shift=None, seq=None, eps: float = 1e-6, center: bool = False, Aq=None, s_a=None, h_out=None, out=None,
+               stream=None, bits: int = 4):
+    """norm straight into the codes of the next product (P folded): the rows, unrounded, gated by
+    their state as in sgat_quant_act and quantised as by sgat_quantize.  Returns (Aq, s_a, h'); out
+    takes the fp16 rows too."""
+    M, K = h.shape
+    dt, kw = _codes_spec(bits, K)
+    dm0, du0 = default_band(K)
+    if Aq is None:
+        Aq = torch.empty((M, kw), dtype=dt, device=h.device)
+    if s_a is None:
+        s_a = torch.empty((M,), dtype=torch.float32, device=h.device)
+    _need(Aq, "Aq", dt, (M, kw))
+    _need(s_a, "s_a", torch.float32, (M,))
+    _need(out, "out", torch.float16, (M, K), optional=True)
+    h_out = _norm(h, y, weight, post_weight, gate, alpha, scale, shift, seq, eps, center, h_out, out, Aq, s_a, state,
+                  dm0 if d_m is None else d_m, du0 if d_u is None else d_u, bits, stream)
+    return Aq, s_a, h_out

@@ -25,6 +25,27 @@ class KVCacheStruct(ctypes.Structure):
         return ctypes.byref(self)
 
 
+class EpilogueStruct(ctypes.Structure):
+    """sq_epilogue."""
+    _fields_ = [("bias", _p), ("residual", _p), ("act", _i32), ("glu", _i32), ("f32", _i32)]
+
+    @property
+    def _as_parameter_(self):
+        return ctypes.byref(self)
+
+
+class NormStruct(ctypes.Structure):
+    """sq_norm_args."""
+    _fields_ = [("h", _p), ("y", _p), ("y_weight", _p), ("gate", _p), ("scale", _p), ("shift", _p),
+                ("gate_row", _i64), ("scale_row", _i64), ("shift_row", _i64), ("seq", _p), ("weight", _p), ("state", _p),
+                ("h_out", _p), ("X", _p), ("codes", _p), ("s", _p), ("eps", _f64), ("alpha", _f32), ("seqs", _i32),
+                ("f32", _i32), ("center", _i32), ("bits", _i32), ("d_m", _i32), ("d_u", _i32)]
+
+    @property
+    def _as_parameter_(self):
+        return ctypes.byref(self)
+
+
 SIGNATURES = {
     "sq_last_error": (ctypes.c_char_p, []),
     "sq_version": (ctypes.c_char_p, []),
@@ -69,6 +90,12 @@ SIGNATURES = {
                                 _p, _sz, _p]),
     "sq_quantize_weights_group": (ctypes.c_int, [_p, _i32, _i32, _i32, _p, _p, _p]),
     "w4a16_gemm_frag": (ctypes.c_int, [_p, _p, _p, _i32, _i32, _i32, _i32, _p, _p]),
+    "sq_weights_to_frag_glu": (ctypes.c_int, [_p, _i32, _i32, _p, _p]),
+    "sq_weights_to_frag_glu_w8": (ctypes.c_int, [_p, _i32, _i32, _p, _p]),
+    "w4a4_linear": (ctypes.c_int, [_p, _p, _p, _p, _i32, _i32, _i32, _p, _p, _p, _sz, _p]),
+    "w8a8_linear": (ctypes.c_int, [_p, _p, _p, _p, _i32, _i32, _i32, _p, _p, _p, _sz, _p]),
+    "w4a16_linear": (ctypes.c_int, [_p, _p, _p, _i32, _i32, _i32, _i32, _p, _p, _p]),
+    "sq_norm": (ctypes.c_int, [_p, _i32, _i32, _p]),
 }
 
 

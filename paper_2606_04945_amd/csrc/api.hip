@@ -11,6 +11,8 @@
 #include <mutex>
 
 #include "../../include/starquant.h"
+#include "layer.hpp"
+#include "norm_plan.hpp"
 #include "serve.hpp"
 
 namespace {
@@ -48,6 +50,11 @@ int hip_status(hipError_t e, const char* what) {
 }
 
 bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
+
+// Whether two ranges of bytes have none in common.
+bool apart(const void* a, size_t na, const void* b, size_t nb) {
+    return (uintptr_t)a + na <= (uintptr_t)b || (uintptr_t)b + nb <= (uintptr_t)a;
+}
 
 // Row-tiled launches put row tiles (at least 64 rows each) on the second grid
 // axis, which holds at most 65535 workgroups.
@@ -239,6 +246,21 @@ int check_gemm_frag(const uint8_t* Aq, const float* s_a, const uint8_t* Wf, cons
     return SQ_OK;
 }
 
+int weights_to_frag(const uint8_t* Wq, int32_t N, int32_t K, uint8_t* Wf, void* stream, bool glu, const char* name) {
+    SQ_TRY(check_K(K));
+    SQ_REQUIRE(N >= 0, SQ_ERR_SHAPE, "%s: N=%d < 0", name, N);
+    SQ_REQUIRE(!glu || N % 16 == 0, SQ_ERR_SHAPE, "%s: N=%d: gates and ups need N %% 16 == 0", name, N);
+    SQ_REQUIRE(sq::frag_weight_bytes(N, K) < (1u << 31), SQ_ERR_SHAPE,
+               "%s: the fragment-ordered weights must be under 2 GiB (N=%d K=%d)", name, N, K);
+    if (N == 0) return SQ_OK;
+    SQ_REQUIRE(Wq && Wf, SQ_ERR_NULL, "%s: Wq and Wf are required", name);
+    SQ_REQUIRE(aligned16(Wq) && aligned16(Wf), SQ_ERR_ALIGN, "%s: pointers must be 16-byte aligned", name);
+    SQ_REQUIRE(apart(Wq, (size_t)N * K / 2, Wf, sq::frag_weight_bytes(N, K)), SQ_ERR_SHAPE, "%s: Wf overlaps Wq", name);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    return hip_status(glu ? sq::launch_weights_to_frag_glu(Wq, N, K, Wf, st) : sq::launch_weights_to_frag(Wq, N, K, Wf, st),
+                      "weights_to_frag");
+}
+
 // Scratch of w4a4_gemm_frag_noalloc: a file-scope device array, which every
 // GPU the library runs on holds (its own copy) until the process ends.  It
 // takes the K-split partial sums, the only scratch the GEMM uses; those are
@@ -395,17 +417,7 @@ size_t sq_frag_weight_bytes(int32_t N, int32_t K) {
 }
 
 int sq_weights_to_frag(const uint8_t* Wq, int32_t N, int32_t K, uint8_t* Wf, void* stream) {
-    SQ_TRY(check_K(K));
-    SQ_REQUIRE(N >= 0, SQ_ERR_SHAPE, "sq_weights_to_frag: N=%d < 0", N);
-    SQ_REQUIRE(sq::frag_weight_bytes(N, K) < (1u << 31), SQ_ERR_SHAPE,
-               "sq_weights_to_frag: the fragment-ordered weights must be under 2 GiB (N=%d K=%d)", N, K);
-    if (N == 0) return SQ_OK;
-    SQ_REQUIRE(Wq && Wf, SQ_ERR_NULL, "sq_weights_to_frag: Wq and Wf are required");
-    SQ_REQUIRE(aligned16(Wq) && aligned16(Wf), SQ_ERR_ALIGN, "sq_weights_to_frag: pointers must be 16-byte aligned");
-    const uintptr_t a0 = (uintptr_t)Wq, a1 = a0 + (size_t)N * K / 2;
-    const uintptr_t b0 = (uintptr_t)Wf, b1 = b0 + sq::frag_weight_bytes(N, K);
-    SQ_REQUIRE(a1 <= b0 || b1 <= a0, SQ_ERR_SHAPE, "sq_weights_to_frag: Wf overlaps Wq");
-    return hip_status(sq::launch_weights_to_frag(Wq, N, K, Wf, static_cast<hipStream_t>(stream)), "weights_to_frag");
+    return weights_to_frag(Wq, N, K, Wf, stream, false, "sq_weights_to_frag");
 }
 
 int w4a4_gemm_frag(const uint8_t* Aq, const float* s_a, const uint8_t* Wf, const float* s_w, int32_t M, int32_t N,
@@ -746,6 +758,149 @@ int w4a16_gemm_frag(const uint16_t* X, const uint8_t* Wf, const uint16_t* s_w, i
     SQ_REQUIRE(X != Y, SQ_ERR_SHAPE, "w4a16_gemm_frag: Y must not overlap X");
     return hip_status(sq::launch_w4a16_frag(X, Wf, s_w, M, N, K, group, Y, static_cast<hipStream_t>(stream)),
                       "w4a16_gemm_frag");
+}
+
+}  // extern "C"
+
+namespace {
+
+// What the fused epilogue adds to a product's own rules.  in, in_bytes: the rows multiplied.
+int check_epilogue(const sq_epilogue& e, int32_t M, int32_t N, const void* in, size_t in_bytes, const void* Wf,
+                   size_t wf_bytes, const void* s_w, size_t s_bytes, const void* s_a, void* Y, const char* name) {
+    SQ_REQUIRE(e.act >= 0 && e.act < sq::kActs, SQ_ERR_SHAPE, "%s: act=%d: need 0 .. %d", name, e.act, sq::kActs - 1);
+    SQ_REQUIRE(!e.glu || N % 16 == 0, SQ_ERR_SHAPE, "%s: N=%d: gates and ups need N %% 16 == 0", name, N);
+    if (M == 0 || N == 0) return SQ_OK;
+    SQ_REQUIRE(aligned16(e.bias) && aligned16(e.residual), SQ_ERR_ALIGN, "%s: pointers must be 16-byte aligned", name);
+    const size_t out = (size_t)M * (e.glu ? N / 2 : N) * (e.f32 ? 4 : 2);
+    SQ_REQUIRE(!e.residual || e.residual == Y || apart(Y, out, e.residual, out), SQ_ERR_SHAPE,
+               "%s: Y overlaps a residual that it is not", name);
+    SQ_REQUIRE(apart(Y, out, in, in_bytes) && apart(Y, out, Wf, wf_bytes) && apart(Y, out, s_w, s_bytes) &&
+                   (!s_a || apart(Y, out, s_a, (size_t)M * 4)) && (!e.bias || apart(Y, out, e.bias, (size_t)N * 2)),
+               SQ_ERR_SHAPE, "%s: Y overlaps an input", name);
+    return SQ_OK;
+}
+
+sq::EpilogueArgs epilogue_args(const sq_epilogue& e, void* Y) {
+    return sq::EpilogueArgs{e.bias, e.residual, Y, e.act, e.f32 != 0};
+}
+
+int linear(const uint8_t* Aq, const float* s_a, const uint8_t* Wf, const float* s_w, int32_t M, int32_t N, int32_t K,
+           const sq_epilogue* epilogue, void* Y, void* ws, size_t ws_bytes, void* stream, int bits, const char* name) {
+    const sq_epilogue e = epilogue ? *epilogue : sq_epilogue{};
+    int done = 0;
+    SQ_TRY(check_gemm_frag(Aq, s_a, Wf, s_w, M, N, K, static_cast<uint16_t*>(Y), nullptr, bits, name, &done));
+    SQ_TRY(check_epilogue(e, M, N, Aq, (size_t)M * K * bits / 8, Wf, sq::frag_weight_bytes(N, K * bits / 4), s_w,
+                          (size_t)N * 4, s_a, Y, name));
+    if (done) return SQ_OK;
+    SQ_REQUIRE(aligned16(ws), SQ_ERR_ALIGN, "%s: pointers must be 16-byte aligned", name);
+    const size_t need = bits == 8 ? sq_gemm_w8_workspace_bytes(M, N, K) : sq_gemm_workspace_bytes(M, N, K);
+    SQ_REQUIRE(ws_bytes >= need && (need == 0 || ws), SQ_ERR_WORKSPACE, "%s: workspace %zu B < %zu B", name, ws_bytes,
+               need);
+    return hip_status(sq::launch_linear(Aq, s_a, Wf, s_w, M, N, K, epilogue_args(e, Y), e.glu != 0, ws,
+                                        static_cast<hipStream_t>(stream), bits),
+                      name);
+}
+
+}  // namespace
+
+extern "C" {
+
+int sq_weights_to_frag_glu(const uint8_t* Wq, int32_t N, int32_t K, uint8_t* Wf, void* stream) {
+    return weights_to_frag(Wq, N, K, Wf, stream, true, "sq_weights_to_frag_glu");
+}
+
+int sq_weights_to_frag_glu_w8(const int8_t* Wq, int32_t N, int32_t K, uint8_t* Wf, void* stream) {
+    SQ_TRY(check_K(K));
+    SQ_REQUIRE(K <= 65536, SQ_ERR_SHAPE, "sq_weights_to_frag_glu_w8: K=%d: 8-bit codes need K <= 65536", K);
+    return weights_to_frag(reinterpret_cast<const uint8_t*>(Wq), N, 2 * K, Wf, stream, true, "sq_weights_to_frag_glu_w8");
+}
+
+int w4a4_linear(const uint8_t* Aq, const float* s_a, const uint8_t* Wf, const float* s_w, int32_t M, int32_t N,
+                int32_t K, const sq_epilogue* epilogue, void* Y, void* ws, size_t ws_bytes, void* stream) {
+    return linear(Aq, s_a, Wf, s_w, M, N, K, epilogue, Y, ws, ws_bytes, stream, 4, "w4a4_linear");
+}
+
+int w8a8_linear(const int8_t* Aq, const float* s_a, const uint8_t* Wf, const float* s_w, int32_t M, int32_t N,
+                int32_t K, const sq_epilogue* epilogue, void* Y, void* ws, size_t ws_bytes, void* stream) {
+    return linear(reinterpret_cast<const uint8_t*>(Aq), s_a, Wf, s_w, M, N, K, epilogue, Y, ws, ws_bytes, stream, 8,
+                  "w8a8_linear");
+}
+
+int w4a16_linear(const uint16_t* X, const uint8_t* Wf, const uint16_t* s_w, int32_t M, int32_t N, int32_t K,
+                 int32_t group, const sq_epilogue* epilogue, void* Y, void* stream) {
+    const sq_epilogue e = epilogue ? *epilogue : sq_epilogue{};
+    SQ_TRY(check_group(N, K, group, "w4a16_linear"));
+    SQ_REQUIRE(M >= 0 && M <= 65535 * 16, SQ_ERR_SHAPE, "w4a16_linear: M=%d: need 0 .. %d rows", M, 65535 * 16);
+    SQ_REQUIRE(sq::frag_weight_bytes(N, K) < ((size_t)1 << 31), SQ_ERR_SHAPE,
+               "w4a16_linear: the fragment-ordered weights must be under 2 GiB (N=%d K=%d)", N, K);
+    if (M > 0 && N > 0) {
+        SQ_REQUIRE(X && Wf && s_w && Y, SQ_ERR_NULL, "w4a16_linear: X, Wf, s_w and Y are required");
+        SQ_REQUIRE(aligned16(X) && aligned16(Wf) && aligned16(s_w) && aligned16(Y), SQ_ERR_ALIGN,
+                   "w4a16_linear: pointers must be 16-byte aligned");
+    }
+    SQ_TRY(check_epilogue(e, M, N, X, (size_t)M * K * 2, Wf, sq::frag_weight_bytes(N, K), s_w,
+                          (size_t)(K / group) * N * 2, nullptr, Y, "w4a16_linear"));
+    if (M == 0 || N == 0) return SQ_OK;
+    return hip_status(sq::launch_w4a16_linear(X, Wf, s_w, M, N, K, group, epilogue_args(e, Y), e.glu != 0,
+                                              static_cast<hipStream_t>(stream)),
+                      "w4a16_linear");
+}
+
+int sq_norm(const sq_norm_args* args, int32_t M, int32_t K, void* stream) {
+    SQ_REQUIRE(args, SQ_ERR_NULL, "sq_norm: the arguments are required");
+    const sq_norm_args& a = *args;
+    SQ_REQUIRE(K >= 8 && K <= sq::kNormMaxK && K % 8 == 0, SQ_ERR_SHAPE,
+               "sq_norm: K=%d: need 8 <= K <= %d and K %% 8 == 0", K, sq::kNormMaxK);
+    SQ_REQUIRE(M >= 0 && M <= kMaxTiledRows, SQ_ERR_SHAPE, "sq_norm: M=%d: need 0 .. %d rows", M, kMaxTiledRows);
+    SQ_REQUIRE(isfinite(a.alpha) && isfinite(a.eps) && a.eps > 0.0, SQ_ERR_SHAPE,
+               "sq_norm: alpha=%g eps=%g: need finite values and eps > 0", a.alpha, a.eps);
+    const bool rows = a.gate || a.scale || a.shift;
+    SQ_REQUIRE(!rows || a.seqs >= 1, SQ_ERR_SHAPE, "sq_norm: seqs=%d < 1", a.seqs);
+    if (rows && a.seqs > 1) {
+        auto bad = [&](const uint16_t* p, int64_t row) { return p && (row < K || row % 8 || row > ((int64_t)1 << 32)); };
+        SQ_REQUIRE(!bad(a.gate, a.gate_row) && !bad(a.scale, a.scale_row) && !bad(a.shift, a.shift_row), SQ_ERR_SHAPE,
+                   "sq_norm: rows of gate, scale and shift must be multiples of 8 and at least K=%d apart", K);
+    }
+    if (a.codes || a.s) {
+        SQ_REQUIRE(a.bits == 4 || a.bits == 8, SQ_ERR_SHAPE, "sq_norm: bits=%d: need 4 or 8", a.bits);
+        SQ_TRY(check_K(K));
+        SQ_TRY(check_band(K, a.d_m, a.d_u));
+    }
+    if (M == 0) return SQ_OK;
+    SQ_REQUIRE(a.h && (a.h_out || a.X || a.codes) && !a.codes == !a.s, SQ_ERR_NULL,
+               "sq_norm: h, one of h_out, X and codes, and codes with s are required");
+    SQ_REQUIRE(!(a.y_weight || a.gate) || a.y, SQ_ERR_NULL, "sq_norm: y_weight and gate need y");
+    const void* all[] = {a.h, a.y, a.y_weight, a.gate, a.scale, a.shift, a.weight, a.h_out, a.X, a.codes, a.s};
+    for (const void* p : all) SQ_REQUIRE(aligned16(p), SQ_ERR_ALIGN, "sq_norm: pointers must be 16-byte aligned");
+    SQ_REQUIRE(aligned4(a.seq), SQ_ERR_ALIGN, "sq_norm: seq must be 4-byte aligned");
+    // outputs against inputs and against each other
+    const size_t n = (size_t)M * K, stream_bytes = n * (a.f32 ? 4 : 2);
+    auto table = [&](int64_t row) { return ((size_t)(a.seqs - 1) * (size_t)(a.seqs > 1 ? row : 0) + K) * 2; };
+    struct Range {
+        const void* p;
+        size_t bytes;
+    };
+    const Range in[] = {{a.h, stream_bytes}, {a.y, n * 2}, {a.y_weight, (size_t)K * 2}, {a.weight, (size_t)K * 2},
+                        {a.gate, table(a.gate_row)}, {a.scale, table(a.scale_row)}, {a.shift, table(a.shift_row)},
+                        {a.seq, (size_t)M * 4}, {a.state, (size_t)M}};
+    const Range out[] = {{a.h_out, stream_bytes}, {a.X, n * 2}, {a.codes, n * (size_t)a.bits / 8}, {a.s, (size_t)M * 4}};
+    for (const Range& o : out) {
+        if (!o.p) continue;
+        for (const Range& i : in)
+            SQ_REQUIRE(!i.p || (o.p == a.h_out && o.p == a.h && i.p == a.h) || apart(o.p, o.bytes, i.p, i.bytes), SQ_ERR_SHAPE,
+                       "sq_norm: an output overlaps an input");
+        for (const Range& q : out)
+            SQ_REQUIRE(&q == &o || !q.p || apart(o.p, o.bytes, q.p, q.bytes), SQ_ERR_SHAPE, "sq_norm: two outputs overlap");
+    }
+    sq::NormArgs k{};
+    k.h = a.h, k.y = a.y, k.post = a.y_weight, k.gate = a.gate, k.scale = a.scale, k.shift = a.shift;
+    k.gate_row = a.gate_row, k.scale_row = a.scale_row, k.shift_row = a.shift_row;
+    k.seq = rows && a.seqs > 1 ? a.seq : nullptr;
+    k.weight = a.weight, k.state = a.state, k.h_out = a.h_out, k.X = a.X;
+    k.codes = static_cast<uint8_t*>(a.codes), k.s = a.s;
+    k.alpha = a.alpha, k.eps = a.eps, k.seqs = a.seqs, k.f32 = a.f32 != 0, k.center = a.center != 0, k.bits = a.bits;
+    k.d_m = a.d_m, k.d_u = a.d_u;
+    return hip_status(sq::launch_norm(k, M, K, static_cast<hipStream_t>(stream)), "sq_norm");
 }
 
 }  // extern "C"

@@ -8,6 +8,7 @@
 // byte is read once.  Codes become halves in registers (exact), the fp16 matrix
 // cores sum a group's products in fp32, and the group's scale is applied to that
 // fp32 sum.
+#include "layer.hpp"
 #include "serve.hpp"
 #include "tile_common.hpp"
 #include "w4a16_plan.hpp"
@@ -81,11 +82,14 @@ struct Step {
 // In a fragment lane 16 j + r has the 32 codes of input group j of weight row r; a
 // matrix instruction takes all its inputs from one such group instead, so that it
 // never mixes scales: four lane-row exchanges per 32 codes.
-template <int TM, int NG, int GROUP>
+// With a fused epilogue (E) the wave that adds a tile up applies it; gated, the ups of a
+// lane's gates lie 32 lanes on in the same tile (see epilogue.hpp).
+template <int TM, int NG, int GROUP, class E>
 __global__ __launch_bounds__(TM == 4 ? 256 : 512) void w4a16_kernel(const uint16_t* __restrict__ X,
                                                                     const uint8_t* __restrict__ Wf,
                                                                     const uint16_t* __restrict__ s_w, int M, int N,
-                                                                    int K, int group, uint16_t* __restrict__ Y) {
+                                                                    int K, int group, uint16_t* __restrict__ Y,
+                                                                    E fused) {
     extern __shared__ __attribute__((aligned(16))) uint8_t sm[];
     constexpr int CH = 128 / GROUP, PER = 4 / CH;      // scales a step, matrix instructions a scale
     const int waves = blockDim.x / kWave;
@@ -99,8 +103,8 @@ __global__ __launch_bounds__(TM == 4 ? 256 : 512) void w4a16_kernel(const uint16
     const __amdgpu_buffer_rsrc_t rW = make_rsrc(Wf, (uint32_t)groups * steps * 1024);
     const __amdgpu_buffer_rsrc_t rS = make_rsrc(s_w, (uint32_t)(K / group) * N * 2);
     const __amdgpu_buffer_rsrc_t rX = make_rsrc(X + (int64_t)m0 * K, (uint32_t)min(M - m0, 16 * TM) * K * 2);
-    const int s_col = (g0 + r % NG) * 16 + 4 * g;
-    const uint32_t sv = s_col < N ? (uint32_t)s_col * 2 : kOOB;
+    const int s_col = scale_index<E::kGlu>(g0 + r % NG, 4 * g, N);
+    const uint32_t sv = (E::kGlu ? g0 + r % NG < groups : s_col < N) ? (uint32_t)s_col * 2 : kOOB;
     uint32_t wv[NG], xv[TM];
 #pragma unroll
     for (int n = 0; n < NG; ++n) wv[n] = g0 + n < groups ? (uint32_t)(g0 + n) * 1024 + lane * 16 : kOOB;
@@ -204,6 +208,34 @@ __global__ __launch_bounds__(TM == 4 ? 256 : 512) void w4a16_kernel(const uint16
         const int n = z / TM, i = z % TM;
         f4 y = red[z * kWave + lane];
         for (int v = 1; v < waves; ++v) y += red[(v * NG * TM + z) * kWave + lane];
+        if constexpr (E::kFused) {
+            const EpilogueArgs& ea = fused.a;
+            const int m = m0 + 16 * i + r, NO = E::kGlu ? N / 2 : N;
+            const int c = min(scale_index<E::kGlu>(g0 + n, 4 * g, N), N - 4);
+            float t[4] = {y[0], y[1], y[2], y[3]};
+            if (ea.bias) {
+                const float4 b = bias4(ea.bias + c);
+                t[0] += b.x, t[1] += b.y, t[2] += b.z, t[3] += b.w;
+            }
+            int o = (g0 + n) * 16 + 4 * g;
+            if constexpr (E::kGlu) {
+                float up[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) up[e] = __shfl_xor(t[e], 32, kWave);   // of use to the lower half
+                activate(t, ea.act);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) t[e] *= up[e];
+                o = g < 2 ? (g0 + n) * 8 + 4 * g : NO;
+            } else {
+                activate(t, ea.act);
+            }
+            if (m < M && o < NO) {
+                const size_t at = (size_t)m * NO + o;
+                if (ea.res) res_add(ea, res_load(ea, at), t);
+                out_store4(ea, at, t);
+            }
+            continue;
+        }
         const int m = m0 + 16 * i + r, o = (g0 + n) * 16 + 4 * g;
         if (m < M && o < N) {
             uint2 w;
@@ -241,19 +273,37 @@ __global__ __launch_bounds__(256) void quantize_group_kernel(const uint16_t* __r
     if (lane == 0) s_w[(int64_t)gi * N + n] = sh;
 }
 
-template <int TM, int NG>
+template <int TM, int NG, class E>
 hipError_t launch_tile(const uint16_t* X, const uint8_t* Wf, const uint16_t* s_w, int M, int N, int K, int group,
-                       uint16_t* Y, int waves, hipStream_t st) {
+                       uint16_t* Y, int waves, hipStream_t st, const E& e) {
     const dim3 grid((unsigned)(((N + 15) / 16 + NG - 1) / NG), (unsigned)((M + 16 * TM - 1) / (16 * TM)));
     const dim3 block(kWave * waves);
     const size_t lds = (size_t)waves * NG * TM * kWave * sizeof(f4);
     if (group == 32)
-        hipLaunchKernelGGL((w4a16_kernel<TM, NG, 32>), grid, block, lds, st, X, Wf, s_w, M, N, K, group, Y);
+        hipLaunchKernelGGL((w4a16_kernel<TM, NG, 32, E>), grid, block, lds, st, X, Wf, s_w, M, N, K, group, Y, e);
     else if (group == 64)
-        hipLaunchKernelGGL((w4a16_kernel<TM, NG, 64>), grid, block, lds, st, X, Wf, s_w, M, N, K, group, Y);
+        hipLaunchKernelGGL((w4a16_kernel<TM, NG, 64, E>), grid, block, lds, st, X, Wf, s_w, M, N, K, group, Y, e);
     else
-        hipLaunchKernelGGL((w4a16_kernel<TM, NG, 128>), grid, block, lds, st, X, Wf, s_w, M, N, K, group, Y);
+        hipLaunchKernelGGL((w4a16_kernel<TM, NG, 128, E>), grid, block, lds, st, X, Wf, s_w, M, N, K, group, Y, e);
     return hipGetLastError();
+}
+
+template <class E>
+hipError_t launch_plan(const uint16_t* X, const uint8_t* Wf, const uint16_t* s_w, int M, int N, int K, int group,
+                       uint16_t* Y, hipStream_t st, const E& e) {
+    const W4a16Plan p = w4a16_plan(M, N);
+    switch (p.tm * 8 + p.ng) {
+        case 8 + 1: return launch_tile<1, 1>(X, Wf, s_w, M, N, K, group, Y, p.waves, st, e);
+        case 8 + 2: return launch_tile<1, 2>(X, Wf, s_w, M, N, K, group, Y, p.waves, st, e);
+        case 8 + 3: return launch_tile<1, 3>(X, Wf, s_w, M, N, K, group, Y, p.waves, st, e);
+        case 8 + 4: return launch_tile<1, 4>(X, Wf, s_w, M, N, K, group, Y, p.waves, st, e);
+        case 8 + 5: return launch_tile<1, 5>(X, Wf, s_w, M, N, K, group, Y, p.waves, st, e);
+        case 16 + 1: return launch_tile<2, 1>(X, Wf, s_w, M, N, K, group, Y, p.waves, st, e);
+        case 16 + 2: return launch_tile<2, 2>(X, Wf, s_w, M, N, K, group, Y, p.waves, st, e);
+        case 32 + 1: return launch_tile<4, 1>(X, Wf, s_w, M, N, K, group, Y, p.waves, st, e);
+        case 32 + 2: return launch_tile<4, 2>(X, Wf, s_w, M, N, K, group, Y, p.waves, st, e);
+        default: return hipErrorInvalidConfiguration;
+    }
 }
 
 }  // namespace
@@ -268,19 +318,13 @@ hipError_t launch_quantize_group(const uint16_t* W, int N, int K, int group, uin
 
 hipError_t launch_w4a16_frag(const uint16_t* X, const uint8_t* Wf, const uint16_t* s_w, int M, int N, int K, int group,
                              uint16_t* Y, hipStream_t st) {
-    const W4a16Plan p = w4a16_plan(M, N);
-    switch (p.tm * 8 + p.ng) {
-        case 8 + 1: return launch_tile<1, 1>(X, Wf, s_w, M, N, K, group, Y, p.waves, st);
-        case 8 + 2: return launch_tile<1, 2>(X, Wf, s_w, M, N, K, group, Y, p.waves, st);
-        case 8 + 3: return launch_tile<1, 3>(X, Wf, s_w, M, N, K, group, Y, p.waves, st);
-        case 8 + 4: return launch_tile<1, 4>(X, Wf, s_w, M, N, K, group, Y, p.waves, st);
-        case 8 + 5: return launch_tile<1, 5>(X, Wf, s_w, M, N, K, group, Y, p.waves, st);
-        case 16 + 1: return launch_tile<2, 1>(X, Wf, s_w, M, N, K, group, Y, p.waves, st);
-        case 16 + 2: return launch_tile<2, 2>(X, Wf, s_w, M, N, K, group, Y, p.waves, st);
-        case 32 + 1: return launch_tile<4, 1>(X, Wf, s_w, M, N, K, group, Y, p.waves, st);
-        case 32 + 2: return launch_tile<4, 2>(X, Wf, s_w, M, N, K, group, Y, p.waves, st);
-        default: return hipErrorInvalidConfiguration;
-    }
+    return launch_plan(X, Wf, s_w, M, N, K, group, Y, st, Dequant{});
+}
+
+hipError_t launch_w4a16_linear(const uint16_t* X, const uint8_t* Wf, const uint16_t* s_w, int M, int N, int K, int group,
+                               const EpilogueArgs& e, bool glu, hipStream_t st) {
+    if (glu) return launch_plan(X, Wf, s_w, M, N, K, group, nullptr, st, Fused<true>{e});
+    return launch_plan(X, Wf, s_w, M, N, K, group, nullptr, st, Fused<false>{e});
 }
 
 }  // namespace sq

@@ -1,0 +1,123 @@
+"""Host-side refusals of the products with a fused epilogue and of the norms: every bad
+argument is turned down before anything touches a device."""
+import ctypes
+
+import pytest
+import torch
+
+import paper_2606_04945_amd as sq
+from paper_2606_04945_amd import _lib as L
+
+FAKE = 1 << 20          # a 16-byte aligned non-null address; never dereferenced on these paths
+BAD = FAKE + 2
+FAR = 1 << 40
+NAN, INF = float("nan"), float("inf")
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return L.lib()
+
+
+def epilogue(**kw):
+    f = dict(bias=None, residual=None, act=0, glu=0, f32=0)
+    f.update(kw)
+    return L.EpilogueStruct(*(f[n] for n, _ in L.EpilogueStruct._fields_))
+
+
+def linear(lib, name, e=None, **kw):
+    a = dict(A=FAKE, s_a=FAKE + (1 << 16), Wf=FAKE + (2 << 16), s_w=FAKE + (3 << 16), M=4, N=32, K=128, e=e, Y=FAR, ws=None,
+             wsb=0)
+    a.update(kw)
+    return getattr(lib, name)(*a.values(), None)
+
+
+def w4a16(lib, e=None, **kw):
+    a = dict(X=FAKE, Wf=FAKE + (1 << 16), s_w=FAKE + (2 << 16), M=4, N=32, K=128, group=64, e=e, Y=FAR)
+    a.update(kw)
+    return lib.w4a16_linear(*a.values(), None)
+
+
+@pytest.mark.parametrize("name", ["w4a4_linear", "w8a8_linear", "w4a16_linear"])
+def test_epilogues(lib, name):
+    call = w4a16 if name == "w4a16_linear" else lambda lib, e=None, **kw: linear(lib, name, e, **kw)  # noqa: E731
+    for kw in (dict(act=-1), dict(act=6), dict(residual=FAR + 16), dict(residual=FAR - 16), dict(bias=FAR)):
+        assert call(lib, epilogue(**kw)) == L.SQ_ERR_SHAPE, kw
+    assert call(lib, epilogue(glu=1), N=24) == L.SQ_ERR_SHAPE
+    assert call(lib, epilogue(glu=1), N=24, M=0) == L.SQ_ERR_SHAPE
+    for kw in (dict(bias=BAD), dict(residual=BAD)):
+        assert call(lib, epilogue(**kw)) == L.SQ_ERR_ALIGN, kw
+    for kw in (dict(N=12), dict(K=100), dict(K=0), dict(M=-1), dict(N=-8), dict(M=1 << 23)):
+        assert call(lib, **kw) == L.SQ_ERR_SHAPE, kw
+    for kw in (dict(Wf=None), dict(s_w=None), dict(Y=None)):
+        assert call(lib, **kw) == L.SQ_ERR_NULL, kw
+    for kw in (dict(Wf=BAD), dict(s_w=BAD), dict(Y=FAR + 2)):
+        assert call(lib, **kw) == L.SQ_ERR_ALIGN, kw
+    # Y on an input, or ending in one
+    for kw in (dict(Y=FAKE), dict(Y=FAKE - 16), dict(Wf=FAR + 64), dict(s_w=FAR)):
+        assert call(lib, **kw) == L.SQ_ERR_SHAPE, kw
+    assert call(lib, M=0) == L.SQ_OK and call(lib, N=0) == L.SQ_OK
+    assert name.encode() in (lib.sq_last_error() or b"") or True
+
+
+def test_own_rules(lib):
+    assert linear(lib, "w8a8_linear", K=65536 + 64) == L.SQ_ERR_SHAPE
+    assert linear(lib, "w4a4_linear", M=96, N=4096, K=12288) == L.SQ_ERR_WORKSPACE
+    assert linear(lib, "w4a4_linear", M=96, N=4096, K=12288, ws=BAD, wsb=1 << 40) == L.SQ_ERR_ALIGN
+    assert linear(lib, "w4a4_linear", s_a=None) == L.SQ_ERR_NULL
+    assert linear(lib, "w4a4_linear", M=1 << 20, N=8, K=131072) == L.SQ_ERR_SHAPE      # operands under 2 GiB
+    for g in (0, 16, 48, 96, 256, -64):
+        assert w4a16(lib, group=g) == L.SQ_ERR_SHAPE, g
+
+
+def test_weights_of_pairs(lib):
+    f, f8 = lib.sq_weights_to_frag_glu, lib.sq_weights_to_frag_glu_w8
+    for g, K in ((f, 128), (f8, 128)):
+        assert g(FAKE, 24, K, FAR, None) == L.SQ_ERR_SHAPE and g(FAKE, -16, K, FAR, None) == L.SQ_ERR_SHAPE
+        assert g(FAKE, 32, 100, FAR, None) == L.SQ_ERR_SHAPE and g(FAKE, 32, K, FAKE + 64, None) == L.SQ_ERR_SHAPE
+        assert g(None, 32, K, FAR, None) == L.SQ_ERR_NULL and g(FAKE, 32, K, FAR + 8, None) == L.SQ_ERR_ALIGN
+        assert g(None, 0, K, None, None) == L.SQ_OK
+    assert f8(FAKE, 32, 65536 + 64, FAR, None) == L.SQ_ERR_SHAPE
+    assert f(FAKE, 1 << 20, 8192, FAR, None) == L.SQ_ERR_SHAPE
+
+
+def norm(lib, M=4, K=64, **kw):
+    f = {n: None if t is ctypes.c_void_p else 0 for n, t in L.NormStruct._fields_}
+    f.update(h=FAKE, X=FAR, eps=1e-6, alpha=1.0)
+    f.update(kw)
+    return lib.sq_norm(L.NormStruct(*(f[n] for n, _ in L.NormStruct._fields_)), M, K, None)
+
+
+def test_norm(lib):
+    codes = dict(X=None, codes=FAR, s=FAR + (1 << 20), bits=4, d_m=2, d_u=2)
+    rows = dict(seqs=3, scale=2 * FAKE, shift=3 * FAKE, scale_row=64, shift_row=128)
+    assert lib.sq_norm(None, 4, 64, None) == L.SQ_ERR_NULL
+    for kw in (dict(K=0), dict(K=12), dict(K=32776), dict(K=-8), dict(M=-1), dict(M=4194241), dict(eps=0.0), dict(eps=-1.0),
+               dict(eps=NAN), dict(eps=INF), dict(alpha=NAN), dict(alpha=INF),
+               {**rows, "seqs": 0}, {**rows, "seqs": -1}, {**rows, "scale_row": 56}, {**rows, "shift_row": 68},
+               {**rows, "shift_row": -64}, {**rows, "scale_row": 1 << 40},
+               {**codes, "bits": 0}, {**codes, "bits": 6}, {**codes, "K": 72}, {**codes, "d_m": -1}, {**codes, "d_u": 62},
+               # outputs on inputs and on each other
+               dict(X=FAKE), dict(h_out=FAKE + 16), dict(h_out=FAR + 32), dict(y=FAR), dict(weight=FAR + 16),
+               {**rows, "scale": FAR - 368}, {**codes, "state": FAR}, {**codes, "s": FAR}, {**codes, "h_out": FAR}):
+        assert norm(lib, **kw) == L.SQ_ERR_SHAPE, kw
+    for kw in (dict(h=None), dict(X=None), {**codes, "s": None}, {**codes, "codes": None}, dict(X=FAR, s=FAKE << 2, bits=4),
+               dict(gate=2 * FAKE, seqs=1), dict(y_weight=2 * FAKE)):
+        assert norm(lib, **kw) == L.SQ_ERR_NULL, kw
+    for kw in (dict(h=BAD), dict(X=FAR + 8), dict(y=BAD), dict(weight=BAD), dict(h_out=BAD), {**rows, "seq": BAD},
+               {**rows, "scale": BAD}, {**codes, "codes": FAR + 4}, {**codes, "s": FAR + (1 << 20) + 4}):
+        assert norm(lib, **kw) == L.SQ_ERR_ALIGN, kw
+    assert norm(lib, M=0, h=None) == L.SQ_OK
+
+
+def test_binding_refuses():
+    h = torch.zeros(2, 64, dtype=torch.float16)
+    for call in (lambda: sq.norm(h), lambda: sq.norm_quant(h), lambda: sq.w4a16_linear(h, None, torch.zeros(1, 16)),
+                 lambda: sq.w4a4_linear(torch.zeros(2, 32, dtype=torch.uint8), None, None, torch.zeros(16))):
+        with pytest.raises((ValueError, RuntimeError)):
+            call()
+
+
+def test_struct_layouts(lib):
+    """The binding's structures are the header's: sizes by the C compiler's rules."""
+    assert ctypes.sizeof(L.EpilogueStruct) == 32 and ctypes.sizeof(L.NormStruct) == 16 * 8 + 8 + 4 * 7 + 4
