@@ -31,7 +31,7 @@ from typing import NamedTuple, Optional, Tuple
 
 import torch
 
-from ._lib import EpilogueStruct, KVCacheStruct, NormStruct, SQ_OK, StarQuantError, check, lib  # noqa: F401
+from ._lib import EPILOGUE, NORM_ARGS, KVCacheStruct, SQ_OK, StarQuantError, check, lib  # noqa: F401
 
 __all__ = ["sgat_prepare_weights", "sgat_transform", "sgat_quantize", "sgat_quant_act", "w4a4_gemm", "tac_apply",
            "tac_default_block", "default_band", "quant_act_workspace_bytes", "gemm_workspace_bytes",
@@ -703,7 +703,11 @@ def w4a16_gemm_frag(X: torch.Tensor, Wf: torch.Tensor, s_w: torch.Tensor, *, Y=N
 
 
 ACTIVATIONS = {"none": 0, "relu": 1, "relu2": 2, "silu": 3, "gelu": 4, "gelu_tanh": 5}
-_FLOATS = (torch.float16, torch.float32)
+_workspace_bytes = functools.lru_cache(maxsize=4096)(gemm_workspace_bytes)      # of sizes alone
+
+
+def _at(t: Optional[torch.Tensor]) -> int:
+    return 0 if t is None else t.data_ptr()
 
 
 def _epilogue(M: int, N: int, like: torch.Tensor, bias, act: str, glu: bool, residual, Y, dtype):
@@ -713,16 +717,18 @@ def _epilogue(M: int, N: int, like: torch.Tensor, bias, act: str, glu: bool, res
     shape = (M, N // 2 if glu else N)
     if dtype is None:
         dtype = Y.dtype if Y is not None else residual.dtype if residual is not None else torch.float16
-    if dtype not in _FLOATS:
+    f32 = dtype is torch.float32
+    if not f32 and dtype is not torch.float16:
         raise ValueError(f"the output must be torch.float16 or torch.float32, got {dtype}")
-    _need(bias, "bias", torch.float16, (N,), optional=True)
-    _need(residual, "residual", dtype, shape, optional=True)
+    if bias is not None:
+        _need(bias, "bias", torch.float16, (N,))
+    if residual is not None:
+        _need(residual, "residual", dtype, shape)
     if Y is None:
-        Y = torch.empty(shape, dtype=dtype, device=like.device)
+        Y = like.new_empty(shape, dtype=dtype)
     else:
         _need(Y, "Y", dtype, shape)
-    return EpilogueStruct(_ptr(bias), _ptr(residual), _choice(ACTIVATIONS, act, "act"), int(glu),
-                          int(dtype is torch.float32)), Y
+    return EPILOGUE.pack(_at(bias), _at(residual), _choice(ACTIVATIONS, act, "act"), bool(glu), f32), Y
 
 
 @_on_stream
@@ -743,9 +749,9 @@ def w4a4_linear(Aq: torch.Tensor, s_a: torch.Tensor, Wf: torch.Tensor, s_w: torc
     _need(s_a, "s_a", torch.float32, (M,))
     _need(s_w, "s_w", torch.float32, (N,))
     e, Y = _epilogue(M, N, Aq, bias, act, glu, residual, Y, dtype)
-    ws, wsb = _ws(gemm_workspace_bytes(M, N, K, bits), ws, Aq.device)
+    ws, wsb = _ws(_workspace_bytes(M, N, K, bits), ws, Aq.device)
     _run(lib().w8a8_linear if bits == 8 else lib().w4a4_linear, (Aq, s_a, Wf, s_w, bias, residual, Y, ws),
-         (_ptr(Aq), _ptr(s_a), _ptr(Wf), _ptr(s_w), M, N, K, e, _ptr(Y), _ptr(ws), wsb), stream)
+         (Aq.data_ptr(), s_a.data_ptr(), Wf.data_ptr(), s_w.data_ptr(), M, N, K, e, Y.data_ptr(), _ptr(ws), wsb), stream)
     return Y
 
 
@@ -767,48 +773,63 @@ def w4a16_linear(X: torch.Tensor, Wf: torch.Tensor, s_w: torch.Tensor, *, bias=N
     _need(s_w, "s_w", torch.float16, (ng, N))
     e, Y = _epilogue(M, N, X, bias, act, glu, residual, Y, dtype)
     _run(lib().w4a16_linear, (X, Wf, s_w, bias, residual, Y),
-         (_ptr(X), _ptr(Wf), _ptr(s_w), M, N, K, K // ng, e, _ptr(Y)), stream)
+         (X.data_ptr(), Wf.data_ptr(), s_w.data_ptr(), M, N, K, K // ng, e, Y.data_ptr()), stream)
     return Y
+
+
+def _conditions(K: int, gate, scale, shift):
+    """(rows, distances between them) of gate, scale and shift, [seqs, K] or [K]; None: not given."""
+    seqs, strides = 0, []
+    for t, name in ((gate, "gate"), (scale, "scale"), (shift, "shift")):
+        if t is None:
+            strides.append(0)
+            continue
+        if not t.is_cuda or t.dtype is not torch.float16 or t.dim() not in (1, 2) or t.shape[-1] != K:
+            raise ValueError(f"{name} must be a torch.float16 device tensor of shape [K={K}] or [seqs, K]")
+        n = t.shape[0] if t.dim() == 2 else 1
+        if t.stride(-1) != 1:
+            raise ValueError(f"{name} must be dense in its last dimension")
+        if n == 0 or (seqs and n != seqs):
+            raise ValueError("gate, scale and shift must have the same number of rows, at least one")
+        seqs = n
+        strides.append(t.stride(0) if t.dim() == 2 else K)
+    return seqs, strides
+
+
+_NO_ROWS = (0, (0, 0, 0))
 
 
 def _norm(h, y, weight, post_weight, gate, alpha, scale, shift, seq, eps, center, h_out, X, codes, s, state, d_m, d_u,
           bits, stream):
     """One sq_norm call on checked outputs; returns h_out (h itself without y)."""
-    M, K = h.shape
+    M, K = shape = h.shape
     dt = h.dtype
-    if dt not in _FLOATS:
+    f32 = dt is torch.float32
+    if not f32 and dt is not torch.float16:
         raise ValueError(f"h must be torch.float16 or torch.float32, got {dt}")
     _need(h, "h", dt)
-    _need(y, "y", torch.float16, (M, K), optional=True)
-    _need(weight, "weight", torch.float16, (K,), optional=True)
-    _need(post_weight, "post_weight", torch.float16, (K,), optional=True)
-    _need(state, "state", torch.uint8, (M,), optional=True)
-    _need(seq, "seq", torch.int32, (M,), optional=True)
-    if y is None and (post_weight is not None or gate is not None):
+    if y is not None:
+        _need(y, "y", torch.float16, shape)
+    elif post_weight is not None or gate is not None:
         raise ValueError("post_weight and gate need y")
-    seqs, strides = None, []
-    for t, name in ((gate, "gate"), (scale, "scale"), (shift, "shift")):
-        if t is None:
-            strides.append(0)
-            continue
-        n = t.shape[0] if t.dim() == 2 else 1
-        if not t.is_cuda or t.dtype is not torch.float16 or t.dim() not in (1, 2) or t.shape[-1] != K:
-            raise ValueError(f"{name} must be a torch.float16 device tensor of shape [K={K}] or [seqs, K]")
-        if t.stride(-1) != 1:
-            raise ValueError(f"{name} must be dense in its last dimension")
-        if n == 0 or (seqs is not None and n != seqs):
-            raise ValueError("gate, scale and shift must have the same number of rows, at least one")
-        seqs = n
-        strides.append(t.stride(0) if t.dim() == 2 else K)
-    if seqs is not None and seqs > 1 and seq is None and M > 0:
+    if weight is not None:
+        _need(weight, "weight", torch.float16, (K,))
+    if post_weight is not None:
+        _need(post_weight, "post_weight", torch.float16, (K,))
+    if state is not None:
+        _need(state, "state", torch.uint8, (M,))
+    if seq is not None:
+        _need(seq, "seq", torch.int32, (M,))
+    seqs, rows = _NO_ROWS if gate is None and scale is None and shift is None else _conditions(K, gate, scale, shift)
+    if seqs > 1 and seq is None and M > 0:
         raise ValueError("seq is required where gate, scale and shift have several rows")
     if h_out is not None:
-        _need(h_out, "h_out", dt, (M, K))
+        _need(h_out, "h_out", dt, shape)
     elif y is not None:
         h_out = torch.empty_like(h)
-    a = NormStruct(_ptr(h), _ptr(y), _ptr(post_weight), _ptr(gate), _ptr(scale), _ptr(shift), *strides, _ptr(seq),
-                   _ptr(weight), _ptr(state), _ptr(h_out), _ptr(X), _ptr(codes), _ptr(s), eps, alpha, seqs or 0,
-                   int(dt is torch.float32), int(center), bits, d_m, d_u)
+    a = NORM_ARGS.pack(h.data_ptr(), _at(y), _at(post_weight), _at(gate), _at(scale), _at(shift), *rows, _at(seq),
+                       _at(weight), _at(state), _at(h_out), _at(X), _at(codes), _at(s), eps, alpha, seqs, f32, bool(center),
+                       bits, d_m, d_u)
     _run(lib().sq_norm, (h, y, weight, post_weight, gate, scale, shift, seq, state, h_out, X, codes, s), (a, M, K), stream)
     return h if h_out is None else h_out
 
@@ -822,13 +843,12 @@ def norm(h: torch.Tensor, y: Optional[torch.Tensor] = None, *, weight=None, post
     + shift, fp16.  RMS norm, or with center=True the mean taken off.  gate, scale and shift are
     [seqs, K] fp16 (rows any multiple of 8 apart) of which token i takes row seq[i], or [K].  Without y
     h' is h.  Returns (X, h'); h_out may be h."""
-    M, K = h.shape
     if out is None:
-        out = torch.empty((M, K), dtype=torch.float16, device=h.device)
-    _need(out, "out", torch.float16, (M, K))
-    h_out = _norm(h, y, weight, post_weight, gate, alpha, scale, shift, seq, eps, center, h_out, out, None, None, None,
-                  0, 0, 0, stream)
-    return out, h_out
+        out = h.new_empty(h.shape, dtype=torch.float16)
+    else:
+        _need(out, "out", torch.float16, h.shape)
+    return out, _norm(h, y, weight, post_weight, gate, alpha, scale, shift, seq, eps, center, h_out, out, None, None, None,
+                      0, 0, 0, stream)
 
 
 @_on_stream
@@ -841,14 +861,16 @@ def norm_quant(h: torch.Tensor, y: Optional[torch.Tensor] = None, *, state=None,
     takes the fp16 rows too."""
     M, K = h.shape
     dt, kw = _codes_spec(bits, K)
-    dm0, du0 = default_band(K)
     if Aq is None:
-        Aq = torch.empty((M, kw), dtype=dt, device=h.device)
+        Aq = h.new_empty((M, kw), dtype=dt)
+    else:
+        _need(Aq, "Aq", dt, (M, kw))
     if s_a is None:
-        s_a = torch.empty((M,), dtype=torch.float32, device=h.device)
-    _need(Aq, "Aq", dt, (M, kw))
-    _need(s_a, "s_a", torch.float32, (M,))
-    _need(out, "out", torch.float16, (M, K), optional=True)
+        s_a = h.new_empty((M,), dtype=torch.float32)
+    else:
+        _need(s_a, "s_a", torch.float32, (M,))
+    if out is not None:
+        _need(out, "out", torch.float16, (M, K))
     h_out = _norm(h, y, weight, post_weight, gate, alpha, scale, shift, seq, eps, center, h_out, out, Aq, s_a, state,
-                  dm0 if d_m is None else d_m, du0 if d_u is None else d_u, bits, stream)
+                  K // 32 if d_m is None else d_m, K // 32 if d_u is None else d_u, bits, stream)
     return Aq, s_a, h_out

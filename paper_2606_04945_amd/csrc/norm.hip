@@ -66,29 +66,41 @@ __device__ __forceinline__ float wave_most(float v) {
     return __builtin_elementwise_maximum(__builtin_bit_cast(float, p0), __builtin_bit_cast(float, p1));
 }
 
-// Sums and maxima over the waves that share a row, each through a place of its own in LDS.
-constexpr int kMaxWaves = 16, kExchanges = 5;
-template <bool SHARED>
+// Sums and maxima over the WAVES waves that share a row, each through a place of its own in LDS.
+constexpr int kExchanges = 7;        // three for each of two norms, one for the largest entry
+template <int WAVES>
 struct Row {
-    double (*red)[kMaxWaves];
-    int wave, waves, lane, used;
+    double (*red)[WAVES];
+    int wave, lane, used;
     __device__ __forceinline__ double sum(double v) {
         v = wave_sum(v);
-        if constexpr (!SHARED) return v;
+        if constexpr (WAVES == 1) return v;
         if (lane == 0) red[used][wave] = v;
         __syncthreads();
         double s = red[used][0];
-        for (int w = 1; w < waves; ++w) s += red[used][w];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) s += red[used][w];
         ++used;
         return s;
     }
+    __device__ __forceinline__ void sum(double& v, double& w) {
+        v = wave_sum(v), w = wave_sum(w);
+        if constexpr (WAVES == 1) return;
+        if (lane == 0) red[used][wave] = v, red[used + 1][wave] = w;
+        __syncthreads();
+        v = red[used][0], w = red[used + 1][0];
+#pragma unroll
+        for (int i = 1; i < WAVES; ++i) v += red[used][i], w += red[used + 1][i];
+        used += 2;
+    }
     __device__ __forceinline__ float most(float v) {
         v = wave_most(v);
-        if constexpr (!SHARED) return v;
+        if constexpr (WAVES == 1) return v;
         if (lane == 0) red[used][wave] = v;
         __syncthreads();
         float s = (float)red[used][0];
-        for (int w = 1; w < waves; ++w) s = __builtin_elementwise_maximum(s, (float)red[used][w]);
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) s = __builtin_elementwise_maximum(s, (float)red[used][w]);
         ++used;
         return s;
     }
@@ -101,252 +113,290 @@ __device__ __forceinline__ void halves(const v4i& raw, float (&x)[8]) {
         x[2 * q] = lo_h(w), x[2 * q + 1] = hi_h(w);
     }
 }
+__device__ __forceinline__ v4i to_halves(const float (&x)[8]) {
+    v4i w;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) w[q] = (int)((uint32_t)f2h(x[2 * q]) | ((uint32_t)f2h(x[2 * q + 1]) << 16));
+    return w;
+}
+
+// A vector of the stream in its own type: what a lane holds of it between the sums.
+template <bool F32>
+struct Held {
+    v4i raw[F32 ? 2 : 1];
+    __device__ __forceinline__ void get(float (&x)[8]) const {
+        if constexpr (F32) {
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                const int b = raw[q / 4][q % 4];       // copied out first: a bit cast of a vector element reads element 0
+                x[q] = __builtin_bit_cast(float, b);
+            }
+        } else {
+            halves(raw[0], x);
+        }
+    }
+    __device__ __forceinline__ void put(const float (&x)[8]) {   // rounds to the stream's type
+        if constexpr (F32) {
+#pragma unroll
+            for (int q = 0; q < 8; ++q) raw[q / 4][q % 4] = __builtin_bit_cast(int, x[q]);
+        } else {
+            raw[0] = to_halves(x);
+        }
+    }
+};
 
 // A lane's vectors of 8 entries: number i is vector lane + i lanes of the row; past the row
-// loads give zeros, so every lane runs the same code.
-template <int NV, bool F32, bool SHARED>
-__global__ __launch_bounds__(SHARED ? 1024 : 64 * kRowsPerGroup) void norm_kernel(NormArgs a, int M, int K) {
-    __shared__ double red[kExchanges][kMaxWaves];
+// loads give zeros, so every lane runs the same code.  FULL: norm of y, gate, scale, shift and
+// means are possible; BITS: of the codes, 0 for none.
+template <int NV, bool F32, int WAVES, bool FULL, int BITS>
+__global__ __launch_bounds__(kWave * (WAVES == 1 ? kRowsPerGroup : WAVES)) void norm_kernel(NormArgs a, int M, int K) {
+    constexpr bool SHARED = WAVES > 1;
+    __shared__ double red[kExchanges][WAVES];
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int row = SHARED ? (int)blockIdx.x : (int)blockIdx.x * kRowsPerGroup + wave;
     if (!SHARED && row >= M) return;
-    const int lanes = SHARED ? blockDim.x : kWave, t = SHARED ? threadIdx.x : lane;
-    Row<SHARED> group{red, wave, (int)blockDim.x / kWave, lane, 0};
+    constexpr int lanes = kWave * WAVES;
+    const int t = SHARED ? threadIdx.x : lane;
+    Row<WAVES> group{red, wave, lane, 0};
+    const bool center = FULL && a.center;
 
     const int64_t at = (int64_t)row * K;
     const uint32_t bytes = (uint32_t)K * 2;
-    int seq = 0;
-    if (a.seq) seq = min(max(a.seq[row], 0), a.seqs - 1);
-    auto rows = [&](const uint16_t* p, int64_t offset) { return make_rsrc(p ? p + offset : p, p ? bytes : 0u); };
+    struct Vectors {
+        v4i raw[NV];
+    };
+    auto load = [&](const uint16_t* p, int i) {
+        return __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(make_rsrc(p, bytes), (t + i * lanes) * 16, 0, 0));
+    };
+    auto request = [&](const uint16_t* p, int64_t offset, Vectors& f) {
+        if (!p) return;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) f.raw[i] = load(p + offset, i);
+    };
+    // Factors are requested ahead of the sum that their use waits for; where a lane holds four vectors of
+    // each of six kinds they would not fit its registers, and are read as they are used.
+    constexpr bool kAhead = !FULL || NV < 4;
+    auto ahead = [&](const uint16_t* p, int64_t offset, Vectors& f) {
+        if (kAhead) request(p, offset, f);
+    };
+    auto factors = [&](const uint16_t* p, int64_t offset, const Vectors& f, int i, float (&w)[8]) {
+        halves(kAhead ? f.raw[i] : load(p + offset, i), w);
+    };
+    Held<F32> h[NV];
+    Vectors y, post, gate, weight, scale, shift;
     const __amdgpu_buffer_rsrc_t rH = F32 ? make_rsrc(static_cast<const float*>(a.h) + at, 2 * bytes)
                                           : make_rsrc(static_cast<const uint16_t*>(a.h) + at, bytes);
-    const __amdgpu_buffer_rsrc_t rY = rows(a.y, at), rP = rows(a.post, 0), rG = rows(a.gate, seq * a.gate_row);
-    const __amdgpu_buffer_rsrc_t rW = rows(a.weight, 0), rS = rows(a.scale, seq * a.scale_row);
-    const __amdgpu_buffer_rsrc_t rB = rows(a.shift, seq * a.shift_row);
-    auto load = [&](const __amdgpu_buffer_rsrc_t& r, int i) {
-        return __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(r, (t + i * lanes) * 16, 0, 0));
-    };
-
-    v4i yr[NV], hr[NV][F32 ? 2 : 1];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        if constexpr (F32) {
-            hr[i][0] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(rH, (t + i * lanes) * 32, 0, 0));
-            hr[i][1] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(rH, (t + i * lanes) * 32 + 16, 0, 0));
-        } else {
-            hr[i][0] = load(rH, i);
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int z = 0; z < (F32 ? 2 : 1); ++z)
+            h[i].raw[z] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(
+                              rH, (t + i * lanes) * (F32 ? 32 : 16) + 16 * z, 0, 0));
+    request(a.y, at, y);
+    int64_t seq = 0;
+    if (FULL && a.seq) seq = min(max(a.seq[row], 0), a.seqs - 1);
+    const bool masked = BITS != 0 && a.state && a.state[row] != 0;
+
+    // Mean (or 0) and r of a row whose vector i is get(i, x); its entries past K are zeros.  With a
+    // mean: both sums in one pass, mean(x^2) - mean^2 where that loses no more than four bits, else the sum of
+    // (x - mean)^2 in another.
+    auto statistics = [&](auto get, float& mean, float& rate) {
+        double s = 0.0, squares = 0.0;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            float x[8];
+            get(i, x);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                const double d = (double)x[q];
+                if (center) s += d;
+                squares = __builtin_fma(d, d, squares);
+            }
         }
-    }
-    if (a.y) {
+        if (!center) {
+            squares = group.sum(squares) / K;
+        } else {
+            group.sum(s, squares);
+            s /= K;
+            squares = squares / K - s * s;
+            if (!(s * s <= 16.0 * squares)) {
+                squares = 0.0;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) yr[i] = load(rY, i);
-    }
-
-    // mean (or 0) and r of rows x, whose entries past K are zeros
-    auto statistics = [&](const float (&x)[NV][8], float& mean, float& rate) {
-        double centre = 0.0, squares = 0.0;
-        if (a.center) {
-            double s = 0.0;
+                for (int i = 0; i < NV; ++i) {
+                    const bool in = (t + i * lanes) * 8 < K;
+                    float x[8];
+                    get(i, x);
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
-#pragma unroll
-                for (int q = 0; q < 8; ++q) s += (double)x[i][q];
-            centre = group.sum(s) / K;
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const bool in = (t + i * lanes) * 8 < K;
-#pragma unroll
-                for (int q = 0; q < 8; ++q) {
-                    const double d = in ? (double)x[i][q] - centre : 0.0;
-                    squares = __builtin_fma(d, d, squares);
+                    for (int q = 0; q < 8; ++q) {
+                        const double d = in ? (double)x[q] - s : 0.0;
+                        squares = __builtin_fma(d, d, squares);
+                    }
                 }
+                squares = group.sum(squares) / K;
             }
-        } else {
-#pragma unroll
-            for (int i = 0; i < NV; ++i)
-#pragma unroll
-                for (int q = 0; q < 8; ++q) squares = __builtin_fma((double)x[i][q], (double)x[i][q], squares);
         }
-        squares = group.sum(squares);
-        mean = (float)centre;
-        rate = (float)(1.0 / __builtin_sqrt(squares / K + a.eps));
+        mean = (float)s;
+        rate = (float)(1.0 / __builtin_sqrt(squares + a.eps));
     };
 
-    float x[NV][8];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        if constexpr (F32) {
-#pragma unroll
-            for (int q = 0; q < 8; ++q) {
-                const int b = hr[i][q / 4][q % 4];
-                x[i][q] = __builtin_bit_cast(float, b);
-            }
-        } else {
-            halves(hr[i][0], x[i]);
-        }
-    }
     if (a.y) {
-        float u[NV][8];
-#pragma unroll
-        for (int i = 0; i < NV; ++i) halves(yr[i], u[i]);
-        if (a.post) {
-            float mean, rate;
-            statistics(u, mean, rate);
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                float w[8];
-                halves(load(rP, i), w);
-#pragma unroll
-                for (int q = 0; q < 8; ++q) u[i][q] = (a.center ? u[i][q] - mean : u[i][q]) * rate * w[q];
-            }
-        }
-        if (a.gate) {
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                float w[8];
-                halves(load(rG, i), w);
-#pragma unroll
-                for (int q = 0; q < 8; ++q) u[i][q] *= w[q];
+        float mean = 0.0f, rate = 1.0f;
+        if (FULL) {
+            ahead(a.gate, seq * a.gate_row, gate);
+            if (a.post) {
+                ahead(a.post, 0, post);
+                statistics([&](int i, float (&x)[8]) { halves(y.raw[i], x); }, mean, rate);
             }
         }
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
+        for (int i = 0; i < NV; ++i) {
+            float x[8], u[8], w[8];
+            halves(y.raw[i], u);
+            if (FULL && a.post) {
+                factors(a.post, 0, post, i, w);
 #pragma unroll
-            for (int q = 0; q < 8; ++q) {
-                x[i][q] += u[i][q] * a.alpha;
-                if (!F32) x[i][q] = h2f(f2h(x[i][q]));
+                for (int q = 0; q < 8; ++q) u[q] = (center ? u[q] - mean : u[q]) * rate * w[q];
             }
+            if (FULL && a.gate) {
+                factors(a.gate, seq * a.gate_row, gate, i, w);
+#pragma unroll
+                for (int q = 0; q < 8; ++q) u[q] *= w[q];
+            }
+            h[i].get(x);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) x[q] += u[q] * a.alpha;
+            h[i].put(x);
+        }
     }
     if (a.h_out) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int v = t + i * lanes;
             if (v * 8 >= K) continue;
-            if constexpr (F32) {
-                float4* p = reinterpret_cast<float4*>(static_cast<float*>(a.h_out) + at + v * 8);
-                p[0] = make_float4(x[i][0], x[i][1], x[i][2], x[i][3]);
-                p[1] = make_float4(x[i][4], x[i][5], x[i][6], x[i][7]);
-            } else {
-                v4i w;
-#pragma unroll
-                for (int q = 0; q < 4; ++q) w[q] = (int)((uint32_t)f2h(x[i][2 * q]) | ((uint32_t)f2h(x[i][2 * q + 1]) << 16));
-                *reinterpret_cast<v4i*>(static_cast<uint16_t*>(a.h_out) + at + v * 8) = w;
-            }
+            v4i* p = F32 ? reinterpret_cast<v4i*>(static_cast<float*>(a.h_out) + at + v * 8)
+                         : reinterpret_cast<v4i*>(static_cast<uint16_t*>(a.h_out) + at + v * 8);
+            p[0] = h[i].raw[0];
+            if (F32) p[1] = h[i].raw[F32 ? 1 : 0];
         }
     }
-    if (!a.X && !a.codes) return;
+    if (BITS == 0 && !a.X) return;
 
+    ahead(a.weight, 0, weight);
+    if (FULL) {
+        ahead(a.scale, seq * a.scale_row, scale);
+        ahead(a.shift, seq * a.shift_row, shift);
+    }
     float mean, rate;
-    statistics(x, mean, rate);
+    statistics([&](int i, float (&x)[8]) { h[i].get(x); }, mean, rate);
+    // the gate keeps columns [0, lim0) and [lim1, K)
+    const int lim0 = a.state ? (masked ? K - a.d_u : K - a.d_m - a.d_u) : K, lim1 = masked ? K : K - a.d_u;
+    float n[NV][8], most = 0.0f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
+        const int v = t + i * lanes;
+        float(&x)[8] = n[i];
+        float w[8];
+        h[i].get(x);
 #pragma unroll
-        for (int q = 0; q < 8; ++q) x[i][q] = (a.center ? x[i][q] - mean : x[i][q]) * rate;
+        for (int q = 0; q < 8; ++q) x[q] = (center ? x[q] - mean : x[q]) * rate;
         if (a.weight) {
-            float w[8];
-            halves(load(rW, i), w);
+            factors(a.weight, 0, weight, i, w);
 #pragma unroll
-            for (int q = 0; q < 8; ++q) x[i][q] *= w[q];
+            for (int q = 0; q < 8; ++q) x[q] *= w[q];
         }
-        if (a.scale) {
-            float w[8];
-            halves(load(rS, i), w);
+        if (FULL && a.scale) {
+            factors(a.scale, seq * a.scale_row, scale, i, w);
 #pragma unroll
-            for (int q = 0; q < 8; ++q) x[i][q] *= 1.0f + w[q];
+            for (int q = 0; q < 8; ++q) x[q] *= 1.0f + w[q];
         }
-        if (a.shift) {
-            float w[8];
-            halves(load(rB, i), w);
+        if (FULL && a.shift) {
+            factors(a.shift, seq * a.shift_row, shift, i, w);
 #pragma unroll
-            for (int q = 0; q < 8; ++q) x[i][q] += w[q];
+            for (int q = 0; q < 8; ++q) x[q] += w[q];
         }
+        if (a.X && v * 8 < K) *reinterpret_cast<v4i*>(a.X + at + v * 8) = to_halves(x);
+        if (BITS == 0) continue;
+        // nearly every vector is kept or dropped whole (a masked row drops its u-band, an unmasked one its m-band)
+        const int c = 8 * v;
+        if ((c >= K) | ((c >= lim0) & (c + 8 <= lim1))) {
+#pragma unroll
+            for (int q = 0; q < 8; ++q) x[q] = 0.0f;
+        } else if ((c + 8 > lim0) & (c < lim1)) {
+#pragma unroll
+            for (int q = 0; q < 8; ++q) x[q] = (c + q < lim0) | (c + q >= lim1) ? x[q] : 0.0f;
+        }
+#pragma unroll
+        for (int q = 0; q < 8; ++q) most = __builtin_elementwise_maximum(most, fabsf(x[q]));
     }
-    if (a.X) {
+    if constexpr (BITS != 0) {
+        constexpr int QMAX = BITS == 4 ? 7 : 127;
+        most = group.most(most);
+        // a row with an entry that is not finite: scale NaN, zero codes
+        const float s = most < __builtin_inff() ? most / (float)QMAX : __builtin_nanf("");
+        const float inv = s > 0.0f ? 1.0f / s : 0.0f;
+        if (t == 0) a.s[row] = s;
+        uint8_t* cr = a.codes + at * BITS / 8;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int v = t + i * lanes;
             if (v * 8 >= K) continue;
-            v4i w;
-#pragma unroll
-            for (int q = 0; q < 4; ++q) w[q] = (int)((uint32_t)f2h(x[i][2 * q]) | ((uint32_t)f2h(x[i][2 * q + 1]) << 16));
-            *reinterpret_cast<v4i*>(a.X + at + v * 8) = w;
-        }
-    }
-    if (!a.codes) return;
-
-    // the gate keeps columns [0, lim0) and [lim1, K)
-    const bool masked = a.state ? a.state[row] != 0 : false;
-    const int lim0 = a.state ? (masked ? K - a.d_u : K - a.d_m - a.d_u) : K, lim1 = masked ? K : K - a.d_u;
-    float most = 0.0f;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int c = (t + i * lanes) * 8;
-#pragma unroll
-        for (int q = 0; q < 8; ++q) {
-            x[i][q] = (c + q < K) & ((c + q < lim0) | (c + q >= lim1)) ? x[i][q] : 0.0f;
-            most = __builtin_elementwise_maximum(most, fabsf(x[i][q]));
-        }
-    }
-    most = group.most(most);
-    // a row with an entry that is not finite: scale NaN, zero codes
-    const bool finite = most < __builtin_inff();
-    const float s = finite ? most / (a.bits == 4 ? 7.0f : 127.0f) : __builtin_nanf("");
-    const float inv = s > 0.0f ? 1.0f / s : 0.0f;
-    if (t == 0) a.s[row] = s;
-    uint8_t* cr = a.codes + (a.bits == 4 ? at / 2 : at);
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int v = t + i * lanes;
-        if (v * 8 >= K) continue;
-        uint32_t lo = 0, hi = 0;
-        if (a.bits == 4) {
+            uint32_t word[BITS / 4] = {};
             if (s > 0.0f) {
                 int c[8];
-                quant_codes8<7>(x[i], s, inv, c);
+                quant_codes8<QMAX>(n[i], s, inv, c);
 #pragma unroll
-                for (int q = 0; q < 8; ++q) lo |= (uint32_t)(c[q] & 15) << (4 * q);
+                for (int q = 0; q < 8; ++q) word[q * BITS / 32] |= (uint32_t)(c[q] & (BITS == 4 ? 15 : 255)) << (BITS * q % 32);
             }
-            reinterpret_cast<uint32_t*>(cr)[v] = lo;
-        } else {
-            if (s > 0.0f) {
-                int c[8];
-                quant_codes8<127>(x[i], s, inv, c);
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    lo |= (uint32_t)(c[q] & 255) << (8 * q);
-                    hi |= (uint32_t)(c[4 + q] & 255) << (8 * q);
-                }
-            }
-            reinterpret_cast<uint2*>(cr)[v] = make_uint2(lo, hi);
+            if (BITS == 4)
+                reinterpret_cast<uint32_t*>(cr)[v] = word[0];
+            else
+                reinterpret_cast<uint2*>(cr)[v] = make_uint2(word[0], word[BITS / 4 - 1]);
         }
     }
 }
 
-template <int NV, bool F32>
-hipError_t launch(const NormArgs& a, int M, int K, int waves, hipStream_t st) {
-    if (waves == 1)
-        hipLaunchKernelGGL((norm_kernel<NV, F32, false>), dim3((M + kRowsPerGroup - 1) / kRowsPerGroup),
-                           dim3(kWave * kRowsPerGroup), 0, st, a, M, K);
+template <int NV, bool F32, int WAVES, bool FULL>
+void launch(const NormArgs& a, int M, int K, hipStream_t st) {
+    const dim3 grid(WAVES == 1 ? (M + kRowsPerGroup - 1) / kRowsPerGroup : M);
+    const dim3 block(kWave * (WAVES == 1 ? kRowsPerGroup : WAVES));
+    if (!a.codes)
+        hipLaunchKernelGGL((norm_kernel<NV, F32, WAVES, FULL, 0>), grid, block, 0, st, a, M, K);
+    else if (a.bits == 4)
+        hipLaunchKernelGGL((norm_kernel<NV, F32, WAVES, FULL, 4>), grid, block, 0, st, a, M, K);
     else
-        hipLaunchKernelGGL((norm_kernel<NV, F32, true>), dim3(M), dim3(kWave * waves), 0, st, a, M, K);
-    return hipGetLastError();
+        hipLaunchKernelGGL((norm_kernel<NV, F32, WAVES, FULL, 8>), grid, block, 0, st, a, M, K);
 }
 
-template <bool F32>
-hipError_t launch_nv(const NormArgs& a, int M, int K, hipStream_t st) {
-    const NormPlan p = norm_plan(M, K);
-    switch (p.nv) {
-        case 1: return launch<1, F32>(a, M, K, p.waves, st);
-        case 2: return launch<2, F32>(a, M, K, p.waves, st);
-        case 4: return launch<4, F32>(a, M, K, p.waves, st);
-        default: return hipErrorInvalidConfiguration;
-    }
+template <int NV, int WAVES>
+hipError_t launch(const NormArgs& a, int M, int K, hipStream_t st) {
+    const bool full = a.post || a.gate || a.scale || a.shift || a.center;
+    if (a.f32 && full)
+        launch<NV, true, WAVES, true>(a, M, K, st);
+    else if (a.f32)
+        launch<NV, true, WAVES, false>(a, M, K, st);
+    else if (full)
+        launch<NV, false, WAVES, true>(a, M, K, st);
+    else
+        launch<NV, false, WAVES, false>(a, M, K, st);
+    return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_norm(const NormArgs& a, int M, int K, hipStream_t st) {
-    return a.f32 ? launch_nv<true>(a, M, K, st) : launch_nv<false>(a, M, K, st);
+    const NormPlan p = norm_plan(M, K);
+    switch (p.waves * 8 + p.nv) {
+        case 8 + 1: return launch<1, 1>(a, M, K, st);
+        case 16 + 1: return launch<1, 2>(a, M, K, st);
+        case 16 + 2: return launch<2, 2>(a, M, K, st);
+        case 32 + 1: return launch<1, 4>(a, M, K, st);
+        case 32 + 2: return launch<2, 4>(a, M, K, st);
+        case 64 + 1: return launch<1, 8>(a, M, K, st);
+        case 64 + 2: return launch<2, 8>(a, M, K, st);
+        case 128 + 2: return launch<2, 16>(a, M, K, st);
+        case 128 + 4: return launch<4, 16>(a, M, K, st);
+        default: return hipErrorInvalidConfiguration;
+    }
 }
 
 }  // namespace sq

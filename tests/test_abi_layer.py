@@ -1,6 +1,7 @@
 """Host-side refusals of the products with a fused epilogue and of the norms: every bad
 argument is turned down before anything touches a device."""
-import ctypes
+import os
+import subprocess
 
 import pytest
 import torch
@@ -20,9 +21,9 @@ def lib():
 
 
 def epilogue(**kw):
-    f = dict(bias=None, residual=None, act=0, glu=0, f32=0)
+    f = dict(bias=0, residual=0, act=0, glu=0, f32=0)
     f.update(kw)
-    return L.EpilogueStruct(*(f[n] for n, _ in L.EpilogueStruct._fields_))
+    return L.EPILOGUE.pack(*(f[n] for n in L.EPILOGUE_FIELDS))
 
 
 def linear(lib, name, e=None, **kw):
@@ -82,10 +83,10 @@ def test_weights_of_pairs(lib):
 
 
 def norm(lib, M=4, K=64, **kw):
-    f = {n: None if t is ctypes.c_void_p else 0 for n, t in L.NormStruct._fields_}
+    f = dict.fromkeys(L.NORM_FIELDS, 0)
     f.update(h=FAKE, X=FAR, eps=1e-6, alpha=1.0)
     f.update(kw)
-    return lib.sq_norm(L.NormStruct(*(f[n] for n, _ in L.NormStruct._fields_)), M, K, None)
+    return lib.sq_norm(L.NORM_ARGS.pack(*(f[n] or 0 for n in L.NORM_FIELDS)), M, K, None)
 
 
 def test_norm(lib):
@@ -118,6 +119,20 @@ def test_binding_refuses():
             call()
 
 
-def test_struct_layouts(lib):
-    """The binding's structures are the header's: sizes by the C compiler's rules."""
-    assert ctypes.sizeof(L.EpilogueStruct) == 32 and ctypes.sizeof(L.NormStruct) == 16 * 8 + 8 + 4 * 7 + 4
+def test_struct_layouts(tmp_path):
+    """The binding packs the header's structures: every field where the C compiler has it."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    lines = []
+    for struct, fields in (("sq_epilogue", L.EPILOGUE_FIELDS), ("sq_norm_args", L.NORM_FIELDS)):
+        lines.append(f'printf("%zu\\n", sizeof({struct}));')
+        lines += [f'printf("%zu %zu\\n", offsetof({struct}, {f}), sizeof((({struct}*)0)->{f}));' for f in fields]
+    (tmp_path / "t.c").write_text('#include <stdio.h>\n#include "starquant.h"\nint main(void) {' + "\n".join(lines)
+                                  + "return 0; }")
+    subprocess.run(["gcc", "-I", os.path.join(root, "include"), str(tmp_path / "t.c"), "-o", str(tmp_path / "t")], check=True)
+    told = iter(subprocess.run([str(tmp_path / "t")], check=True, capture_output=True, text=True).stdout.splitlines())
+    for packer, fields in ((L.EPILOGUE, L.EPILOGUE_FIELDS), (L.NORM_ARGS, L.NORM_FIELDS)):
+        assert packer.size == int(next(told))
+        for i, f in enumerate(fields):
+            at, size = map(int, next(told).split())
+            one = packer.pack(*(1.0 if j == i and f in ("eps", "alpha") else int(j == i) for j in range(len(fields))))
+            assert any(one[at:at + size]) and not any(one[:at]) and not any(one[at + size:]), f

@@ -74,6 +74,37 @@ def test_widths(K, f32):
     check(Case(rng, 3, K, f32, post=True, gate=True, mod=True, seqs=4), center=True)
 
 
+@pytest.mark.parametrize("K", [1032, 2048, 2056, 4096])
+@pytest.mark.parametrize("f32", [False, True], ids=["fp16", "fp32"])
+def test_many_rows_of_middle_widths(K, f32):
+    """More rows than the plan's borders, which take another share of a row a wave."""
+    rng = np.random.default_rng(K)
+    M = 1100
+    c = Case(rng, M, K, f32, post=True, gate=True, mod=True, seqs=4)
+    check(c, center=True)
+    c = Case(rng, M, K, f32)
+    n, h = check(c)
+    state = (rng.random(M) < 0.5).astype(np.uint8)
+    if K % 64 == 0:
+        for bits in (4, 8):
+            q, s = L.quantise(L.gated(n, state, K // 32, K // 32), bits)
+            Aq, s_a, _ = sq.norm_quant(dev(c.h), dev(c.y), state=dev(state), bits=bits, **c.device_kw(alpha=0.5))
+            assert_bits(host(Aq), q, "codes")
+            assert_bits(host(s_a), s, "scales")
+
+
+@pytest.mark.parametrize("M,K", [(5, 520), (5, 4096), (600, 4096), (5, 20000)])
+@pytest.mark.parametrize("spread", [2.0 ** -9, 2.0 ** -4, 0.26, 1.0])
+def test_means_far_from_zero(M, K, spread):
+    """Rows whose mean is many times their spread: the sum of squares takes a second pass there."""
+    rng = np.random.default_rng(K)
+    c = Case(rng, M, K, True, post=True)
+    c.h = (1 + spread * rng.normal(0, 1, (M, K))).astype(np.float32)
+    c.h[0] = 1.0
+    c.y = (1 + spread * rng.normal(0, 1, (M, K))).astype(np.float16)
+    check(c, center=True)
+
+
 OPTIONS = [dict(), dict(add=False), dict(weight=False), dict(post=True), dict(gate=True), dict(gate=True, seqs=5),
            dict(mod=True, seqs=3), dict(mod=True, add=False), dict(post=True, gate=True, mod=True, seqs=7),
            dict(add=False, weight=False)]
