@@ -515,7 +515,7 @@ int w4a16_gemm_frag(const uint16_t* X, const uint8_t* Wf, const uint16_t* s_w, i
  *   bias     [N] fp16, or NULL.
  *   residual [M][N or N / 2] of Y's type, or NULL; it may be Y itself.
  *   f32      non-zero: Y and residual are fp32, else fp16.
- *   Y        dense; apart from `residual` it overlaps no input.
+ *   Y        dense, at most 2^22 outputs a row; apart from `residual` it overlaps no input.
  * The other arguments, rules and workspace are those of w4a4_gemm_frag, w8a8_gemm_frag
  * (sq_gemm_workspace_bytes, sq_gemm_w8_workspace_bytes for the same M, N, K) and
  * w4a16_gemm_frag (which needs none; s_w [K / group][N]).  A NULL epilogue is one of zeros.

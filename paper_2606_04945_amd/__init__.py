@@ -316,6 +316,7 @@ def frag_weight_bytes(N: int, K: int, bits: int = 4) -> int:
     return n
 
 
+@functools.lru_cache(maxsize=4096)
 def _frag_shape(N: int, K: int, bits: int):
     step = 64 if bits == 8 else 128
     return ((K + step - 1) // step, (N + 15) // 16, 1024)

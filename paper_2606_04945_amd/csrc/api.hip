@@ -769,6 +769,8 @@ int check_epilogue(const sq_epilogue& e, int32_t M, int32_t N, const void* in, s
                    size_t wf_bytes, const void* s_w, size_t s_bytes, const void* s_a, void* Y, const char* name) {
     SQ_REQUIRE(e.act >= 0 && e.act < sq::kActs, SQ_ERR_SHAPE, "%s: act=%d: need 0 .. %d", name, e.act, sq::kActs - 1);
     SQ_REQUIRE(!e.glu || N % 16 == 0, SQ_ERR_SHAPE, "%s: N=%d: gates and ups need N %% 16 == 0", name, N);
+    // a tile's rows of outputs are addressed with 32-bit buffer offsets
+    SQ_REQUIRE((e.glu ? N / 2 : N) <= 1 << 22, SQ_ERR_SHAPE, "%s: N=%d: at most 2^22 outputs a row", name, N);
     if (M == 0 || N == 0) return SQ_OK;
     SQ_REQUIRE(aligned16(e.bias) && aligned16(e.residual), SQ_ERR_ALIGN, "%s: pointers must be 16-byte aligned", name);
     const size_t out = (size_t)M * (e.glu ? N / 2 : N) * (e.f32 ? 4 : 2);

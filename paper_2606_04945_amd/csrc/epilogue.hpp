@@ -11,7 +11,7 @@
 //                 scales and bias keep the order [gates, ups]: a group's products of one
 //                 row then lie in one wave, gate and up a fixed number of lanes apart.
 #pragma once
-#include "sq_internal.hpp"
+#include "tile_common.hpp"
 
 namespace sq {
 
@@ -69,75 +69,115 @@ __device__ __forceinline__ float over_exp2(float t, float p) {
     return t * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(p));
 }
 
-// act(t), four at a time: `act` is the same for all, so one branch serves them.
-// silu(t) = t / (1 + exp2(-t log2 e));  gelu_tanh(t) = t (1 + tanh u) / 2 = t / (1 + e^(-2u)),
+// act(t).  silu(t) = t / (1 + exp2(-t log2 e));  gelu_tanh(t) = t (1 + tanh u) / 2 = t / (1 + e^(-2u)),
 // u = sqrt(2 / pi) (t + 0.044715 t^3).
-__device__ __forceinline__ void activate(float (&t)[4], int act) {
-    if (act == kActSilu) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) t[e] = over_exp2(t[e], t[e] * -1.44269504f);
-    } else if (act == kActGeluTanh) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) t[e] = over_exp2(t[e], t[e] * __builtin_fmaf(t[e] * t[e], -0.102943240f, -2.30220820f));
-    } else if (act == kActGelu) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) t[e] = gelu_erf(t[e]);
-    } else if (act != kActNone) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float r = t[e] < 0.0f ? 0.0f : t[e];      // a NaN stays one
-            t[e] = act == kActRelu2 ? r * r : r;
-        }
+template <int ACT>
+__device__ __forceinline__ float activated(float t) {
+    if constexpr (ACT == kActSilu) return over_exp2(t, t * -1.44269504f);
+    if constexpr (ACT == kActGeluTanh) return over_exp2(t, t * __builtin_fmaf(t * t, -0.102943240f, -2.30220820f));
+    if constexpr (ACT == kActGelu) return gelu_erf(t);
+    if constexpr (ACT == kActRelu || ACT == kActRelu2) {
+        const float r = t < 0.0f ? 0.0f : t;             // a NaN stays one
+        return ACT == kActRelu2 ? r * r : r;
+    }
+    return t;
+}
+
+template <int ACT>
+struct ActIs {
+    static constexpr int value = ACT;
+};
+// f with the activation as a constant, so that one branch serves a whole epilogue.
+template <class F>
+__device__ __forceinline__ void with_act(int act, F f) {
+    switch (act) {
+        case kActRelu: f(ActIs<kActRelu>()); break;
+        case kActRelu2: f(ActIs<kActRelu2>()); break;
+        case kActSilu: f(ActIs<kActSilu>()); break;
+        case kActGelu: f(ActIs<kActGelu>()); break;
+        case kActGeluTanh: f(ActIs<kActGeluTanh>()); break;
+        default: f(ActIs<kActNone>()); break;
     }
 }
 
-// Four consecutive entries of the residual, as read and as values.
-struct Res4 {
-    uint4 raw;
-};
-__device__ __forceinline__ Res4 res_load(const EpilogueArgs& a, size_t o) {
-    Res4 r{make_uint4(0, 0, 0, 0)};
-    if (a.f32) {
-        r.raw = *reinterpret_cast<const uint4*>(static_cast<const float*>(a.res) + o);
-    } else {
-        const uint2 h = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(a.res) + o);
-        r.raw.x = h.x, r.raw.y = h.y;
+// Rows of the residual, or of Y, as buffers: what lies past the last row or output is read as zeros
+// and not written, and so is a residual that is not there, so nothing branches and the loads
+// of an epilogue are in flight together.  Offsets are of entries, in 32 bits: a caller's rows
+// times their length stay below 2^29 (the host limits N).
+struct RowsBuffer {
+    __amdgpu_buffer_rsrc_t r;
+    int shift;                                           // log2 of an entry's bytes
+    // from row `row0` on, `rows` of them (none if negative) of `length` entries
+    __device__ __forceinline__ RowsBuffer(const void* p, int f32, int row0, int rows, int length) {
+        shift = f32 ? 2 : 1;
+        const uint8_t* base = static_cast<const uint8_t*>(p);
+        if (p) base += ((size_t)row0 * length) << shift;
+        r = make_rsrc(base, p && rows > 0 ? (uint32_t)(rows * length) << shift : 0u);
     }
-    return r;
+};
+// Adding this leaves every value as it is, a zero's sign too.
+__device__ __forceinline__ float neutral_if(bool none, float v) {
+    return __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, v) | (none ? 0x80000000u : 0u));
+}
+
+// Four consecutive entries of the residual, as read.
+struct Res4 {
+    uint2 lo, hi;                                        // fp16: lo; fp32: both
+};
+__device__ __forceinline__ uint2 load_b64(const __amdgpu_buffer_rsrc_t& r, uint32_t at) {
+    return __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(r, (int)at, 0, 0));
+}
+__device__ __forceinline__ Res4 res_load(const RowsBuffer& b, uint32_t entry, bool in) {
+    const uint32_t at = in ? entry << b.shift : kOOB;
+    return Res4{load_b64(b.r, at), load_b64(b.r, b.shift == 2 ? at + 8 : kOOB)};
 }
 __device__ __forceinline__ void res_add(const EpilogueArgs& a, const Res4& r, float (&y)[4]) {
-    if (a.f32) {
-        y[0] += __builtin_bit_cast(float, r.raw.x), y[1] += __builtin_bit_cast(float, r.raw.y);
-        y[2] += __builtin_bit_cast(float, r.raw.z), y[3] += __builtin_bit_cast(float, r.raw.w);
-    } else {
-        y[0] += h2f((uint16_t)(r.raw.x & 0xFFFFu)), y[1] += h2f((uint16_t)(r.raw.x >> 16));
-        y[2] += h2f((uint16_t)(r.raw.y & 0xFFFFu)), y[3] += h2f((uint16_t)(r.raw.y >> 16));
-    }
+    const bool f32 = a.f32, none = a.res == nullptr;
+    const float v0 = f32 ? __builtin_bit_cast(float, r.lo.x) : lo_h(r.lo.x);
+    const float v1 = f32 ? __builtin_bit_cast(float, r.lo.y) : hi_h(r.lo.x);
+    const float v2 = f32 ? __builtin_bit_cast(float, r.hi.x) : lo_h(r.lo.y);
+    const float v3 = f32 ? __builtin_bit_cast(float, r.hi.y) : hi_h(r.lo.y);
+    y[0] += neutral_if(none, v0), y[1] += neutral_if(none, v1);
+    y[2] += neutral_if(none, v2), y[3] += neutral_if(none, v3);
 }
-__device__ __forceinline__ void out_store4(const EpilogueArgs& a, size_t o, const float (&y)[4]) {
-    if (a.f32) {
-        *reinterpret_cast<float4*>(static_cast<float*>(a.Y) + o) = make_float4(y[0], y[1], y[2], y[3]);
+__device__ __forceinline__ void out_store4(const RowsBuffer& b, uint32_t entry, bool in, const float (&y)[4]) {
+    const uint32_t at = in ? entry << b.shift : kOOB;
+    if (b.shift == 2) {
+        v4i w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = __builtin_bit_cast(int, y[e]);
+        __builtin_amdgcn_raw_buffer_store_b128(w, b.r, (int)at, 0, 0);
     } else {
         const uint32_t y0 = f2h(y[0]), y1 = f2h(y[1]), y2 = f2h(y[2]), y3 = f2h(y[3]);
-        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.Y) + o) = make_uint2(y0 | (y1 << 16), y2 | (y3 << 16));
+        typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+        __builtin_amdgcn_raw_buffer_store_b64(u2{y0 | (y1 << 16), y2 | (y3 << 16)}, b.r, (int)at, 0, 0);
     }
 }
 
-// One entry.
-__device__ __forceinline__ float res_one(const EpilogueArgs& a, size_t o) {
-    return a.f32 ? static_cast<const float*>(a.res)[o] : h2f(static_cast<const uint16_t*>(a.res)[o]);
+// One entry: as a word that holds it (rows are of an even number of entries), then as a value.
+__device__ __forceinline__ uint32_t res_load_one(const RowsBuffer& b, uint32_t entry, bool in) {
+    return (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(b.r, (int)(in ? (entry << b.shift) & ~3u : kOOB), 0, 0);
 }
-__device__ __forceinline__ void out_store_one(const EpilogueArgs& a, size_t o, float y) {
-    if (a.f32)
-        static_cast<float*>(a.Y)[o] = y;
+__device__ __forceinline__ float res_one(const EpilogueArgs& a, uint32_t word, uint32_t entry) {
+    const float h = entry & 1 ? hi_h(word) : lo_h(word);
+    return neutral_if(a.res == nullptr, a.f32 ? __builtin_bit_cast(float, word) : h);
+}
+__device__ __forceinline__ void out_store_one(const RowsBuffer& b, uint32_t entry, bool in, float y) {
+    const uint32_t at = in ? entry << b.shift : kOOB;
+    if (b.shift == 2)
+        __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, y), b.r, (int)at, 0, 0);
     else
-        static_cast<uint16_t*>(a.Y)[o] = f2h(y);
+        __builtin_amdgcn_raw_buffer_store_b16(f2h(y), b.r, (int)at, 0, 0);
 }
 
-__device__ __forceinline__ float4 bias4(const uint16_t* b) {
-    const uint2 h = *reinterpret_cast<const uint2*>(b);
-    return make_float4(h2f((uint16_t)(h.x & 0xFFFFu)), h2f((uint16_t)(h.x >> 16)), h2f((uint16_t)(h.y & 0xFFFFu)),
-                       h2f((uint16_t)(h.y >> 16)));
+// Four entries of the bias from a buffer of it (an empty one where there is none).
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t bias_buffer(const EpilogueArgs& a, int N) {
+    return make_rsrc(a.bias, a.bias ? (uint32_t)N * 2 : 0u);
+}
+__device__ __forceinline__ void bias_add(const EpilogueArgs& a, const uint2& h, float (&t)[4]) {
+    const bool none = a.bias == nullptr;
+    t[0] += neutral_if(none, lo_h(h.x)), t[1] += neutral_if(none, hi_h(h.x));
+    t[2] += neutral_if(none, lo_h(h.y)), t[3] += neutral_if(none, hi_h(h.y));
 }
 
 // The partner's value 32 lanes away: on return a and b hold, in lanes 0 .. 31, what a held there and what a

@@ -79,7 +79,8 @@ __device__ __forceinline__ int acc_value(int raw) {   // 4-bit operands carry a 
 // one per set), so a workgroup that owns a whole tile has KG times the waves;
 // the sets' partial sums meet in LDS (exact integer adds) before the epilogue.
 template <class E, int WM, int WN, int TM, int TN, bool SPLIT, int BITS, int OCC, bool WF = false, int KG = 1>
-__global__ __launch_bounds__(64 * WM * WN * KG) __attribute__((amdgpu_waves_per_eu(OCC))) void gemm_tile_kernel(
+__global__ __launch_bounds__(64 * WM * WN * KG) __attribute__((amdgpu_waves_per_eu(
+    E::kFused && WM * WN == 8 ? 4 : OCC))) void gemm_tile_kernel(
     const uint8_t* __restrict__ Aq, const float* __restrict__ s_a, const uint8_t* __restrict__ Wq,
     const float* __restrict__ s_w, int M, int N, int K, int ksteps_per_split, uint16_t* __restrict__ Y,
     int32_t* __restrict__ acc_out, int32_t* __restrict__ part, E fused) {
@@ -258,74 +259,148 @@ __global__ __launch_bounds__(64 * WM * WN * KG) __attribute__((amdgpu_waves_per_
     // of the block's group of 16.  Gated, lanes of lg 0 and 1 have gates and those of lg 2
     // and 3 the ups of the same outputs: exchanging halves of wave between blocks j and
     // j + 1 gives the lower lanes block j's gates and ups and the upper ones block j + 1's.
-    // The residual of a row of blocks is requested one row ahead of its use.
-    auto fused_epilogue = [&](auto NOWRAP) {
+    // What is to be stored takes the place of the sums, then goes through LDS, so that residual and output
+    // are accessed in whole lines: 16 rows of 32 or 64 bytes an instruction keep the address
+    // units busy for as long as the products (16384 x 4096 x 4096 with a residual 262 -> 232 us,
+    // 1000 x 4096 x 4096 onto an fp32 stream 24.2 -> 22.3; without either the products take 209 and 18.8).
+    auto fused_epilogue = [&]() {
         if constexpr (E::kFused && !SPLIT) {
             constexpr bool G = E::kGlu;
             constexpr int ST = G ? 2 : 1;                // blocks that make one block of outputs
-            constexpr int JC = TN < 4 ? TN : 4;          // blocks whose scales, bias and residual are held at a time
+            // (where registers are short: nothing is requested ahead of the step that uses it; a few of
+            // them are kept in memory between the steps all the same, never in the loop over k)
+            constexpr bool kTight = TM * TN > 16 || WM * WN == 8;
             const EpilogueArgs& ea = fused.a;
-            const int NO = G ? N / 2 : N;                // outputs a row
+            const int grp0 = col0 / 16 + wn * TN;
+            const int first = row0 + wm * TM * 16;
+            // scales and bias through buffers: past the last weight row they are zeros
+            const __amdgpu_buffer_rsrc_t bS = make_rsrc(s_w, (uint32_t)N * 4), bB = bias_buffer(ea, N);
             float sa[TM];
 #pragma unroll
-            for (int i = 0; i < TM; ++i) sa[i] = s_a[min(row0 + (wm * TM + i) * 16 + lr, M - 1)];
+            for (int i = 0; i < TM; ++i) sa[i] = s_a[min(first + i * 16 + lr, M - 1)];
+            if (BITS == 4) {                             // the sums, without the operands' factors
+                if (K < 131072) {
 #pragma unroll
-            for (int jc = 0; jc < TN; jc += JC) {
-                const int grp0 = (col0 + wn * TN * 16) / 16 + jc;
-                float4 sw[JC], bi[JC];
-                int oc[JC / ST];                         // this lane's first output column, or past the last
+                    for (int i = 0; i < TM; ++i)
 #pragma unroll
-                for (int j = 0; j < JC; ++j) {
-                    const int c = min(scale_index<G>(grp0 + j, 4 * lg, N), N - 4);
-                    sw[j] = *reinterpret_cast<const float4*>(s_w + c);
-                    if (ea.bias) bi[j] = bias4(ea.bias + c);
+                        for (int j = 0; j < TN; ++j) acc[i][j] >>= 8;
+                } else {
+#pragma unroll
+                    for (int i = 0; i < TM; ++i)
+#pragma unroll
+                        for (int j = 0; j < TN; ++j)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) acc[i][j][e] = acc_value<4>(acc[i][j][e]);
                 }
+            }
+            with_act(ea.act, [&](auto act) {
+                constexpr int A = decltype(act)::value;
 #pragma unroll
-                for (int j = 0; j < JC; j += ST)
-                    oc[j / ST] = G ? 8 * (grp0 + j + lg / 2) + 4 * (lg % 2) : 16 * (grp0 + j) + 4 * lg;
-                Res4 res[2][JC / ST];
-                auto request = [&](int i, Res4 (&r)[JC / ST]) {
-                    const int row = row0 + (wm * TM + i) * 16 + lr;
+                for (int j = 0; j < TN; j += ST) {
+                    if (kTight) __builtin_amdgcn_sched_barrier(0);
+                    v4i sw[ST];
+                    uint2 bias[ST];
 #pragma unroll
-                    for (int j = 0; j < JC; j += ST)
-                        if (ea.res && owns(i, jc + j) && row < M && oc[j / ST] < NO)
-                            r[j / ST] = res_load(ea, (size_t)row * NO + oc[j / ST]);
-                };
-                request(0, res[0]);
+                    for (int z = 0; z < ST; ++z) {
+                        const uint32_t c = (uint32_t)scale_index<G>(grp0 + j + z, 4 * lg, N);
+                        sw[z] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(bS, (int)(c * 4), 0, 0));
+                        bias[z] = load_b64(bB, c * 2);
+                    }
 #pragma unroll
-                for (int i = 0; i < TM; ++i) {
-                    if (i + 1 < TM) request(i + 1, res[(i + 1) % 2]);
-                    const int row = row0 + (wm * TM + i) * 16 + lr;
-#pragma unroll
-                    for (int j = 0; j < JC; j += ST) {
-                        if (!owns(i, jc + j)) continue;
+                    for (int i = 0; i < TM; ++i) {
+                        if (!owns(i, j)) continue;
                         float t[ST][4];
 #pragma unroll
                         for (int z = 0; z < ST; ++z) {
-                            const float w4[4] = {sw[j + z].x, sw[j + z].y, sw[j + z].z, sw[j + z].w};
-                            const float b4[4] = {bi[j + z].x, bi[j + z].y, bi[j + z].z, bi[j + z].w};
 #pragma unroll
                             for (int e = 0; e < 4; ++e) {
-                                const int raw = acc[i][jc + j + z][e];
-                                const int v = decltype(NOWRAP)::value && BITS == 4 ? raw >> 8 : acc_value<BITS>(raw);
-                                t[z][e] = ((float)v * sa[i]) * w4[e];
-                                if (ea.bias) t[z][e] += b4[e];
+                                const int b = sw[z][e];
+                                t[z][e] = ((float)acc[i][j + z][e] * sa[i]) * __builtin_bit_cast(float, b);
                             }
+                            bias_add(ea, bias[z], t[z]);
                         }
                         if constexpr (G) {
 #pragma unroll
                             for (int e = 0; e < 4; ++e) pair_halves(t[0][e], t[1][e]);
                         }
-                        activate(t[0], ea.act);
-                        if constexpr (G) {
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) t[0][e] *= t[1][e];
+                        for (int e = 0; e < 4; ++e) {
+                            t[0][e] = activated<A>(t[0][e]);
+                            if constexpr (G) t[0][e] *= t[1][e];
+                            acc[i][j][e] = __builtin_bit_cast(int, t[0][e]);
                         }
-                        if (ea.res) res_add(ea, res[i % 2][j / ST], t[0]);
-                        if (row < M && oc[j / ST] < NO) out_store4(ea, (size_t)row * NO + oc[j / ST], t[0]);
                     }
                 }
-            }
+            });
+            // The wave's outputs [rows][OC] as floats in LDS, CH blocks of 16 rows at a time: its own
+            // area, or with k groups the one that the groups of these outputs fill together.
+            constexpr int OC = 16 * TN / ST, PITCH = OC + 4, CH = KG > 1 ? TM : kTight ? 1 : 2;
+            static_assert(TM % CH == 0 && NW * CH * 16 * PITCH * 4 <= 3 * SB, "the outputs fit in the stages");
+            float* area = reinterpret_cast<float*>(sm) + wave * CH * 16 * PITCH;
+            const int NO = N / ST, c0 = G ? 8 * grp0 : 16 * grp0;
+            const RowsBuffer bR(ea.res, ea.f32, first, min(M - first, 16 * TM), NO);
+            const RowsBuffer bY(ea.Y, ea.f32, first, min(M - first, 16 * TM), NO);
+            auto finish = [&](auto wide) {               // 4 fp32 or 8 fp16 entries a lane
+                constexpr bool F32 = decltype(wide)::value;
+                constexpr int VE = F32 ? 4 : 8, LPR = OC / VE, RPI = kWave / LPR;   // lanes a row, rows an instruction
+                constexpr int IN = (CH * 16 / RPI + KG - 1) / KG;                   // instructions of a wave
+                const int lrow = lane / LPR, lcol = VE * (lane % LPR);
+#pragma unroll
+                for (int ic = 0; ic < TM; ic += CH) {
+                    if (kTight) __builtin_amdgcn_sched_barrier(0);
+                    v4i r[IN];
+                    uint32_t at[IN];
+#pragma unroll
+                    for (int q = 0; q < IN; ++q) {
+                        const int row = (q * KG + kg) * RPI + lrow;
+                        const bool in = row < CH * 16 && c0 + lcol < NO;
+                        at[q] = in ? (uint32_t)((ic * 16 + row) * NO + c0 + lcol) << (F32 ? 2 : 1) : kOOB;
+                        r[q] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(bR.r, (int)at[q], 0, 0));
+                    }
+#pragma unroll
+                    for (int i = 0; i < CH; ++i)
+#pragma unroll
+                        for (int j = 0; j < TN; j += ST) {
+                            if (!owns(ic + i, j)) continue;
+                            const int c = G ? 8 * (j + lg / 2) + 4 * (lg % 2) : 16 * j + 4 * lg;
+                            *reinterpret_cast<v4i*>(area + (i * 16 + lr) * PITCH + c) = acc[ic + i][j];
+                        }
+                    if (KG > 1)
+                        __syncthreads();
+                    else
+                        asm volatile("" ::: "memory");   // (a wave's LDS accesses stay in order)
+#pragma unroll
+                    for (int q = 0; q < IN; ++q) {
+                        const int row = min((q * KG + kg) * RPI + lrow, CH * 16 - 1);
+                        const float4* p = reinterpret_cast<const float4*>(area + row * PITCH + lcol);
+                        const float4 lo = p[0];
+                        float y[VE] = {lo.x, lo.y, lo.z, lo.w};
+                        if constexpr (!F32) {
+                            const float4 hi = p[1];
+                            y[4] = hi.x, y[5] = hi.y, y[6] = hi.z, y[7] = hi.w;
+                        }
+                        const bool none = ea.res == nullptr;
+                        v4i w;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const uint32_t b = (uint32_t)r[q][e];
+                            if constexpr (F32) {
+                                w[e] = __builtin_bit_cast(int, y[e] + neutral_if(none, __builtin_bit_cast(float, b)));
+                            } else {
+                                const uint32_t y0 = f2h(y[2 * e] + neutral_if(none, lo_h(b)));
+                                const uint32_t y1 = f2h(y[2 * e + 1] + neutral_if(none, hi_h(b)));
+                                w[e] = (int)(y0 | (y1 << 16));
+                            }
+                        }
+                        __builtin_amdgcn_raw_buffer_store_b128(w, bY.r, (int)at[q], 0, 0);
+                    }
+                    asm volatile("" ::: "memory");
+                }
+            };
+            if (ea.f32)
+                finish(std::true_type{});
+            else
+                finish(std::false_type{});
         }
     };
 
@@ -369,7 +444,7 @@ __global__ __launch_bounds__(64 * WM * WN * KG) __attribute__((amdgpu_waves_per_
             for (int j = 0; j < TN; ++j)
                 if (!owns(i, j)) red[slot(kg, i, j)] = acc[i][j];
         __syncthreads();
-        if (kg >= TM * TN) return;
+        if (!E::kFused && kg >= TM * TN) return;
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
@@ -381,10 +456,8 @@ __global__ __launch_bounds__(64 * WM * WN * KG) __attribute__((amdgpu_waves_per_
             }
     }
     if constexpr (E::kFused && !SPLIT) {
-        if (K < 131072)
-            fused_epilogue(std::true_type{});
-        else
-            fused_epilogue(std::false_type{});
+        __syncthreads();                                 // every wave is past its last read of the stages
+        fused_epilogue();
     } else if (K < 131072) {
         epilogue(std::true_type{});
     } else {
@@ -435,57 +508,63 @@ __device__ __forceinline__ void skinny_store(const v4i& acc, int row0, int lg, i
 // The fused epilogue of the short-M kernels: lane (c, g) has rows 16 i + 4 g .. + 3 of weight
 // row c of its group.  Gated, the partner eight lanes away has the other factor of the
 // same outputs; the lanes of gates finish the first two of the four rows, those of ups the
-// other two.  Bias and residual are requested while the weights stream (the residual by the
-// waves that store).
+// other two.  Bias and residual are requested while the weights stream.
 template <class E, int TM>
-struct ShortResidual {
+struct ShortEpilogue {
     static constexpr int R = E::kGlu ? 2 : 4;            // rows of each four that this lane finishes
-    float bias, res[TM][4];
+    uint32_t res[TM][R];
+    float bias;
     __device__ __forceinline__ static int column(int grp, int lr) { return E::kGlu ? 8 * grp + lr % 8 : 16 * grp + lr; }
     __device__ __forceinline__ static int row(int i, int r, int lr, int lg) {
         return 16 * i + 4 * lg + (E::kGlu && lr >= 8 ? 2 : 0) + r;
     }
-    __device__ __forceinline__ void request(const E& f, int grp, int lr, int lg, int M, int N, bool stores) {
+    __device__ __forceinline__ void request(const E& f, int grp, int lr, int lg, int M, int N) {
         if constexpr (E::kFused) {
             const int NO = E::kGlu ? N / 2 : N, col = column(grp, lr);
-            bias = f.a.bias ? h2f(f.a.bias[min(scale_index<E::kGlu>(grp, lr, N), N - 1)]) : 0.0f;
-            if (f.a.res && stores && col < NO) {
+            const uint32_t at = (uint32_t)scale_index<E::kGlu>(grp, lr, N) * 2;
+            const uint32_t word = (uint32_t)__builtin_amdgcn_raw_buffer_load_b16(bias_buffer(f.a, N), (int)at, 0, 0);
+            bias = neutral_if(f.a.bias == nullptr, lo_h(word));
+            const RowsBuffer b(f.a.res, f.a.f32, 0, M, NO);
 #pragma unroll
-                for (int i = 0; i < TM; ++i)
+            for (int i = 0; i < TM; ++i)
 #pragma unroll
-                    for (int r = 0; r < R; ++r)
-                        if (row(i, r, lr, lg) < M) res[i][r] = res_one(f.a, (size_t)row(i, r, lr, lg) * NO + col);
-            }
+                for (int r = 0; r < R; ++r)
+                    res[i][r] = res_load_one(b, (uint32_t)(row(i, r, lr, lg) * NO + col), col < NO && row(i, r, lr, lg) < M);
         }
     }
-    __device__ __forceinline__ void store(const E& f, float (&t)[4], int i, int grp, int lr, int lg, int M, int N) const {
+    __device__ __forceinline__ void store(const E& f, float (&t)[TM][4], int grp, int lr, int lg, int M, int N) const {
         if constexpr (E::kFused) {
             const int NO = E::kGlu ? N / 2 : N, col = column(grp, lr);
-            if (f.a.bias) {
+            const RowsBuffer b(f.a.Y, f.a.f32, 0, M, NO);
+            with_act(f.a.act, [&](auto act) {
+                constexpr int A = decltype(act)::value;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) t[r] += bias;
-            }
-            if constexpr (E::kGlu) {
-                float gate[4], up[4];
-                const bool low = lr < 8;
+                for (int i = 0; i < TM; ++i) {
+                    float y[4];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const float other = row_other_half(t[r]);
-                    gate[r] = low ? t[r] : other, up[r] = low ? other : t[r];
+                    for (int r = 0; r < 4; ++r) y[r] = t[i][r] + bias;
+                    if constexpr (E::kGlu) {
+                        const bool low = lr < 8;
+                        float other[4];
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) other[r] = row_other_half(y[r]);
+#pragma unroll
+                        for (int r = 0; r < 2; ++r) {
+                            const float gate = low ? y[r] : other[r + 2], up = low ? other[r] : y[r + 2];
+                            y[r] = activated<A>(gate) * up;
+                        }
+                    } else {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) y[r] = activated<A>(y[r]);
+                    }
+#pragma unroll
+                    for (int r = 0; r < R; ++r) {
+                        const int m = row(i, r, lr, lg);
+                        const uint32_t at = (uint32_t)(m * NO + col);
+                        out_store_one(b, at, col < NO && m < M, y[r] + res_one(f.a, res[i][r], at));
+                    }
                 }
-                float y[4] = {low ? gate[0] : gate[2], low ? gate[1] : gate[3], 0.0f, 0.0f};
-                activate(y, f.a.act);
-                t[0] = y[0] * (low ? up[0] : up[2]), t[1] = y[1] * (low ? up[1] : up[3]);
-            } else {
-                activate(t, f.a.act);
-            }
-            if (col >= NO) return;
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                const int m = row(i, r, lr, lg);
-                if (m >= M) continue;
-                out_store_one(f.a, (size_t)m * NO + col, f.a.res ? t[r] + res[i][r] : t[r]);
-            }
+            });
         }
     }
 };
@@ -572,8 +651,8 @@ __global__ __launch_bounds__(ALDS ? 1024 : 512) void gemm_short_frag_kernel(
 #pragma unroll
         for (int r = 0; r < 4; ++r) sav[i][r] = s_a[min(16 * i + 4 * lg + r, M - 1)];
     const float swv = s_w[E::kGlu ? min(scale_index<true>(grp, lr, N), N - 1) : min(col, N - 1)];
-    ShortResidual<E, TM> extra;
-    extra.request(fused, grp, lr, lg, M, N, kw == 0);
+    ShortEpilogue<E, TM> extra;
+    extra.request(fused, grp, lr, lg, M, N);
     v4i acc[TM];
 #pragma unroll
     for (int i = 0; i < TM; ++i) acc[i] = v4i{0, 0, 0, 0};
@@ -618,13 +697,12 @@ __global__ __launch_bounds__(ALDS ? 1024 : 512) void gemm_short_frag_kernel(
             for (int i = 0; i < TM; ++i) acc[i] += red[((r * CG + cgi) * TM + i) * kWave + lane];
     }
     if constexpr (E::kFused) {
+        float t[TM][4];
 #pragma unroll
-        for (int i = 0; i < TM; ++i) {
-            float t[4];
+        for (int i = 0; i < TM; ++i)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) t[r] = ((float)acc_value<BITS>(acc[i][r]) * sav[i][r]) * swv;
-            extra.store(fused, t, i, grp, lr, lg, M, N);
-        }
+            for (int r = 0; r < 4; ++r) t[i][r] = ((float)acc_value<BITS>(acc[i][r]) * sav[i][r]) * swv;
+        extra.store(fused, t, grp, lr, lg, M, N);
     } else {
 #pragma unroll
         for (int i = 0; i < TM; ++i) skinny_store<BITS>(acc[i], 16 * i, lg, col, M, N, sav[i], swv, Y, acc_out);
@@ -641,38 +719,37 @@ __global__ __launch_bounds__(256) void splitk_epilogue(const int32_t* __restrict
     if constexpr (E::kFused) {
         // four outputs a thread
         const EpilogueArgs& ea = fused.a;
-        const int NO = E::kGlu ? N / 2 : N, quads = NO / 4;
+        constexpr int Z = E::kGlu ? 2 : 1;
+        const int NO = N / Z, quads = NO / 4;
+        const RowsBuffer bR(ea.res, ea.f32, 0, M, NO), bY(ea.Y, ea.f32, 0, M, NO);
+        const __amdgpu_buffer_rsrc_t bB = bias_buffer(ea, N);
         for (size_t q = (size_t)blockIdx.x * 256 + threadIdx.x; q < (size_t)M * quads; q += (size_t)gridDim.x * 256) {
             const int row = (int)(q / quads), c = 4 * (int)(q % quads);
-            const size_t o = (size_t)row * NO + c;
-            Res4 res;
-            if (ea.res) res = res_load(ea, o);
-            float t[E::kGlu ? 2 : 1][4];
+            const uint32_t o = (uint32_t)(row * NO + c);
+            const Res4 res = res_load(bR, o, true);
+            const float sa = s_a[row];
+            float t[Z][4];
 #pragma unroll
-            for (int z = 0; z < (E::kGlu ? 2 : 1); ++z) {
+            for (int z = 0; z < Z; ++z) {
                 // the sums lie in the order of the weight rows, scales and bias in that of the outputs
-                const int w = E::kGlu ? 16 * (c / 8) + 8 * z + c % 8 : c, s = E::kGlu ? c + z * NO : c;
-                int4 v = make_int4(0, 0, 0, 0);
-                for (int k = 0; k < splits; ++k) {
-                    const int4 p = *reinterpret_cast<const int4*>(part + (size_t)k * total + (size_t)row * N + w);
-                    v.x += p.x, v.y += p.y, v.z += p.z, v.w += p.w;
-                }
+                const int w = E::kGlu ? 16 * (c / 8) + 8 * z + c % 8 : c, s = c + z * NO;
+                v4i v = v4i{0, 0, 0, 0};
+                for (int k = 0; k < splits; ++k)
+                    v += *reinterpret_cast<const v4i*>(part + (size_t)k * total + (size_t)row * N + w);
                 const float4 sw = *reinterpret_cast<const float4*>(s_w + s);
-                const float sa = s_a[row];
-                t[z][0] = ((float)v.x * sa) * sw.x, t[z][1] = ((float)v.y * sa) * sw.y;
-                t[z][2] = ((float)v.z * sa) * sw.z, t[z][3] = ((float)v.w * sa) * sw.w;
-                if (ea.bias) {
-                    const float4 b = bias4(ea.bias + s);
-                    t[z][0] += b.x, t[z][1] += b.y, t[z][2] += b.z, t[z][3] += b.w;
-                }
+                t[z][0] = ((float)v[0] * sa) * sw.x, t[z][1] = ((float)v[1] * sa) * sw.y;
+                t[z][2] = ((float)v[2] * sa) * sw.z, t[z][3] = ((float)v[3] * sa) * sw.w;
+                bias_add(ea, load_b64(bB, (uint32_t)s * 2), t[z]);
             }
-            activate(t[0], ea.act);
-            if constexpr (E::kGlu) {
+            with_act(ea.act, [&](auto act) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) t[0][e] *= t[1][e];
-            }
-            if (ea.res) res_add(ea, res, t[0]);
-            out_store4(ea, o, t[0]);
+                for (int e = 0; e < 4; ++e) {
+                    t[0][e] = activated<decltype(act)::value>(t[0][e]);
+                    if constexpr (E::kGlu) t[0][e] *= t[1][e];
+                }
+            });
+            res_add(ea, res, t[0]);
+            out_store4(bY, o, true, t[0]);
         }
         return;
     }

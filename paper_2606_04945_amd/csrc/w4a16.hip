@@ -197,43 +197,52 @@ __global__ __launch_bounds__(TM == 4 ? 256 : 512) void w4a16_kernel(const uint16
             if (t + 2 * waves >= steps) break;
         }
     }
+    // the waves share the adding up: of the NG TM tiles, number z to wave z % waves; what a fused epilogue
+    // reads is requested ahead of it (tile z's as well as that of tile z + waves, the last)
+    constexpr int kTiles = 2, ST = E::kGlu ? 2 : 1;
+    static_assert(NG * TM <= 4 * kTiles, "at least four waves");
+    const int NO = N / ST, rows = min(M - m0, 16 * TM);
+    Res4 res[kTiles];
+    uint2 bias[kTiles];
+    if constexpr (E::kFused) {
+        const RowsBuffer b(fused.a.res, fused.a.f32, m0, rows, NO);
+        const __amdgpu_buffer_rsrc_t bB = bias_buffer(fused.a, N);
+#pragma unroll
+        for (int u = 0; u < kTiles; ++u) {
+            const int z = wave + u * waves, n = z / TM, i = z % TM;
+            const int o = E::kGlu ? (g < 2 ? (g0 + n) * 8 + 4 * g : NO) : (g0 + n) * 16 + 4 * g;
+            res[u] = res_load(b, (uint32_t)((16 * i + r) * NO + o), z < NG * TM && o < NO);
+            bias[u] = load_b64(bB, (uint32_t)scale_index<E::kGlu>(g0 + n, 4 * g, N) * 2);
+        }
+    }
     f4* red = reinterpret_cast<f4*>(sm);               // [wave][NG][TM][lane]
 #pragma unroll
     for (int n = 0; n < NG; ++n)
 #pragma unroll
         for (int i = 0; i < TM; ++i) red[((wave * NG + n) * TM + i) * kWave + lane] = sum[n][i];
     __syncthreads();
-    // the waves share the adding up: of the NG TM tiles, number z to wave z % waves
-    for (int z = wave; z < NG * TM; z += waves) {
+    for (int z = wave, u = 0; z < NG * TM; z += waves, ++u) {
         const int n = z / TM, i = z % TM;
         f4 y = red[z * kWave + lane];
         for (int v = 1; v < waves; ++v) y += red[(v * NG * TM + z) * kWave + lane];
         if constexpr (E::kFused) {
-            const EpilogueArgs& ea = fused.a;
-            const int m = m0 + 16 * i + r, NO = E::kGlu ? N / 2 : N;
-            const int c = min(scale_index<E::kGlu>(g0 + n, 4 * g, N), N - 4);
             float t[4] = {y[0], y[1], y[2], y[3]};
-            if (ea.bias) {
-                const float4 b = bias4(ea.bias + c);
-                t[0] += b.x, t[1] += b.y, t[2] += b.z, t[3] += b.w;
-            }
-            int o = (g0 + n) * 16 + 4 * g;
+            bias_add(fused.a, u ? bias[1] : bias[0], t);
+            float up[4];
             if constexpr (E::kGlu) {
-                float up[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) up[e] = __shfl_xor(t[e], 32, kWave);   // of use to the lower half
-                activate(t, ea.act);
+            }
+            with_act(fused.a.act, [&](auto act) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) t[e] *= up[e];
-                o = g < 2 ? (g0 + n) * 8 + 4 * g : NO;
-            } else {
-                activate(t, ea.act);
-            }
-            if (m < M && o < NO) {
-                const size_t at = (size_t)m * NO + o;
-                if (ea.res) res_add(ea, res_load(ea, at), t);
-                out_store4(ea, at, t);
-            }
+                for (int e = 0; e < 4; ++e) {
+                    t[e] = activated<decltype(act)::value>(t[e]);
+                    if constexpr (E::kGlu) t[e] *= up[e];
+                }
+            });
+            const int o = E::kGlu ? (g < 2 ? (g0 + n) * 8 + 4 * g : NO) : (g0 + n) * 16 + 4 * g;
+            res_add(fused.a, u ? res[1] : res[0], t);
+            out_store4(RowsBuffer(fused.a.Y, fused.a.f32, m0, rows, NO), (uint32_t)((16 * i + r) * NO + o), o < NO, t);
             continue;
         }
         const int m = m0 + 16 * i + r, o = (g0 + n) * 16 + 4 * g;
