@@ -257,8 +257,9 @@ int weights_to_frag(const uint8_t* Wq, int32_t N, int32_t K, uint8_t* Wf, void* 
     SQ_REQUIRE(aligned16(Wq) && aligned16(Wf), SQ_ERR_ALIGN, "%s: pointers must be 16-byte aligned", name);
     SQ_REQUIRE(apart(Wq, (size_t)N * K / 2, Wf, sq::frag_weight_bytes(N, K)), SQ_ERR_SHAPE, "%s: Wf overlaps Wq", name);
     hipStream_t st = static_cast<hipStream_t>(stream);
-    return hip_status(glu ? sq::launch_weights_to_frag_glu(Wq, N, K, Wf, st) : sq::launch_weights_to_frag(Wq, N, K, Wf, st),
-                      "weights_to_frag");
+    return hip_status(
+        glu ? sq::launch_weights_to_frag_glu(Wq, N, K, Wf, st) : sq::launch_weights_to_frag(Wq, N, K, Wf, st),
+        "weights_to_frag");
 }
 
 // Scratch of w4a4_gemm_frag_noalloc: a file-scope device array, which every
@@ -814,7 +815,8 @@ int sq_weights_to_frag_glu(const uint8_t* Wq, int32_t N, int32_t K, uint8_t* Wf,
 int sq_weights_to_frag_glu_w8(const int8_t* Wq, int32_t N, int32_t K, uint8_t* Wf, void* stream) {
     SQ_TRY(check_K(K));
     SQ_REQUIRE(K <= 65536, SQ_ERR_SHAPE, "sq_weights_to_frag_glu_w8: K=%d: 8-bit codes need K <= 65536", K);
-    return weights_to_frag(reinterpret_cast<const uint8_t*>(Wq), N, 2 * K, Wf, stream, true, "sq_weights_to_frag_glu_w8");
+    return weights_to_frag(reinterpret_cast<const uint8_t*>(Wq), N, 2 * K, Wf, stream, true,
+                           "sq_weights_to_frag_glu_w8");
 }
 
 int w4a4_linear(const uint8_t* Aq, const float* s_a, const uint8_t* Wf, const float* s_w, int32_t M, int32_t N,
@@ -854,12 +856,15 @@ int sq_norm(const sq_norm_args* args, int32_t M, int32_t K, void* stream) {
     SQ_REQUIRE(K >= 8 && K <= sq::kNormMaxK && K % 8 == 0, SQ_ERR_SHAPE,
                "sq_norm: K=%d: need 8 <= K <= %d and K %% 8 == 0", K, sq::kNormMaxK);
     SQ_REQUIRE(M >= 0 && M <= kMaxTiledRows, SQ_ERR_SHAPE, "sq_norm: M=%d: need 0 .. %d rows", M, kMaxTiledRows);
-    SQ_REQUIRE(isfinite(a.alpha) && isfinite(a.eps) && a.eps > 0.0, SQ_ERR_SHAPE,
-               "sq_norm: alpha=%g eps=%g: need finite values and eps > 0", a.alpha, a.eps);
+    // (1 / sqrt(eps), the r of a row of zeros, is finite in fp32)
+    SQ_REQUIRE(isfinite(a.alpha) && isfinite(a.eps) && a.eps >= 1e-30, SQ_ERR_SHAPE,
+               "sq_norm: alpha=%g eps=%g: need finite values and eps >= 1e-30", a.alpha, a.eps);
     const bool rows = a.gate || a.scale || a.shift;
     SQ_REQUIRE(!rows || a.seqs >= 1, SQ_ERR_SHAPE, "sq_norm: seqs=%d < 1", a.seqs);
     if (rows && a.seqs > 1) {
-        auto bad = [&](const uint16_t* p, int64_t row) { return p && (row < K || row % 8 || row > ((int64_t)1 << 32)); };
+        auto bad = [&](const uint16_t* p, int64_t row) {
+            return p && (row < K || row % 8 || row > ((int64_t)1 << 32));
+        };
         SQ_REQUIRE(!bad(a.gate, a.gate_row) && !bad(a.scale, a.scale_row) && !bad(a.shift, a.shift_row), SQ_ERR_SHAPE,
                    "sq_norm: rows of gate, scale and shift must be multiples of 8 and at least K=%d apart", K);
     }
@@ -885,14 +890,16 @@ int sq_norm(const sq_norm_args* args, int32_t M, int32_t K, void* stream) {
     const Range in[] = {{a.h, stream_bytes}, {a.y, n * 2}, {a.y_weight, (size_t)K * 2}, {a.weight, (size_t)K * 2},
                         {a.gate, table(a.gate_row)}, {a.scale, table(a.scale_row)}, {a.shift, table(a.shift_row)},
                         {a.seq, (size_t)M * 4}, {a.state, (size_t)M}};
-    const Range out[] = {{a.h_out, stream_bytes}, {a.X, n * 2}, {a.codes, n * (size_t)a.bits / 8}, {a.s, (size_t)M * 4}};
+    const Range out[] = {{a.h_out, stream_bytes}, {a.X, n * 2}, {a.codes, a.codes ? n * (size_t)a.bits / 8 : 0},
+                         {a.s, (size_t)M * 4}};
     for (const Range& o : out) {
         if (!o.p) continue;
         for (const Range& i : in)
-            SQ_REQUIRE(!i.p || (o.p == a.h_out && o.p == a.h && i.p == a.h) || apart(o.p, o.bytes, i.p, i.bytes), SQ_ERR_SHAPE,
-                       "sq_norm: an output overlaps an input");
+            SQ_REQUIRE(!i.p || (&o == out && &i == in && o.p == i.p) || apart(o.p, o.bytes, i.p, i.bytes), SQ_ERR_SHAPE,
+                       "sq_norm: an output overlaps an input");       // (h_out may be h)
         for (const Range& q : out)
-            SQ_REQUIRE(&q == &o || !q.p || apart(o.p, o.bytes, q.p, q.bytes), SQ_ERR_SHAPE, "sq_norm: two outputs overlap");
+            SQ_REQUIRE(&q == &o || !q.p || apart(o.p, o.bytes, q.p, q.bytes), SQ_ERR_SHAPE,
+                       "sq_norm: two outputs overlap");
     }
     sq::NormArgs k{};
     k.h = a.h, k.y = a.y, k.post = a.y_weight, k.gate = a.gate, k.scale = a.scale, k.shift = a.shift;

@@ -94,13 +94,15 @@ def test_norm(lib):
     codes = dict(X=None, codes=FAR, s=FAR + (1 << 20), bits=4, d_m=2, d_u=2)
     rows = dict(seqs=3, scale=2 * FAKE, shift=3 * FAKE, scale_row=64, shift_row=128)
     assert lib.sq_norm(None, 4, 64, None) == L.SQ_ERR_NULL
-    for kw in (dict(K=0), dict(K=12), dict(K=32776), dict(K=-8), dict(M=-1), dict(M=4194241), dict(eps=0.0), dict(eps=-1.0),
+    for kw in (dict(K=0), dict(K=12), dict(K=32776), dict(K=-8), dict(M=-1), dict(M=4194241), dict(eps=0.0), dict(eps=1e-31),
+               dict(eps=-1.0),
                dict(eps=NAN), dict(eps=INF), dict(alpha=NAN), dict(alpha=INF),
                {**rows, "seqs": 0}, {**rows, "seqs": -1}, {**rows, "scale_row": 56}, {**rows, "shift_row": 68},
                {**rows, "shift_row": -64}, {**rows, "scale_row": 1 << 40},
                {**codes, "bits": 0}, {**codes, "bits": 6}, {**codes, "K": 72}, {**codes, "d_m": -1}, {**codes, "d_u": 62},
                # outputs on inputs and on each other
-               dict(X=FAKE), dict(h_out=FAKE + 16), dict(h_out=FAR + 32), dict(y=FAR), dict(weight=FAR + 16),
+               dict(X=FAKE), dict(h_out=FAKE + 16), dict(h_out=FAKE, y=FAKE), dict(h_out=FAKE, y=FAKE, f32=1),
+               dict(h_out=FAKE, weight=FAKE), dict(h_out=FAR + 32), dict(y=FAR), dict(weight=FAR + 16),
                {**rows, "scale": FAR - 368}, {**codes, "state": FAR}, {**codes, "s": FAR}, {**codes, "h_out": FAR}):
         assert norm(lib, **kw) == L.SQ_ERR_SHAPE, kw
     for kw in (dict(h=None), dict(X=None), {**codes, "s": None}, {**codes, "codes": None}, dict(X=FAR, s=FAKE << 2, bits=4),

@@ -151,3 +151,25 @@ def test_empty():
     assert sq.w4a4_linear(z(0, 64), z(0, dt=f), z(1, 2, 1024), z(32, dt=f), glu=True, act="silu").shape == (0, 16)
     assert sq.w4a4_linear(z(3, 64), z(3, dt=f), z(1, 0, 1024), z(0, dt=f), dtype=f).shape == (3, 0)
     assert sq.w4a16_linear(z(0, 128, dt=torch.float16), z(1, 1, 1024), z(2, 16, dt=torch.float16)).shape == (0, 16)
+
+
+@pytest.mark.parametrize("f32", [False, True], ids=["fp16", "fp32"])
+def test_offsets_past_31_bits(f32):
+    """Outputs and residuals of more than 2^31 entries: the last rows are those of a call of their own."""
+    M, N, K = 140001, 16400, 64
+    g = torch.Generator(device="cuda").manual_seed(1)
+    byte = lambda *s: torch.randint(0, 256, s, generator=g, device="cuda", dtype=torch.uint8)  # noqa: E731
+    A_, W = byte(M, K // 2), byte(N, K // 2)
+    s_a, s_w = (torch.rand(n, generator=g, device="cuda") * 0.1 + 0.01 for n in (M, N))
+    bias = torch.randn(N, generator=g, device="cuda").to(torch.float16)
+    dtype = torch.float32 if f32 else torch.float16
+    tail = torch.randn(300, N, generator=g, device="cuda").to(dtype)
+    Y = torch.zeros(M, N, device="cuda", dtype=dtype)
+    Y[-300:] = tail
+    Wf = sq.weights_to_frag(W)
+    got = sq.w4a4_linear(A_, s_a, Wf, s_w, bias=bias, act="relu", residual=Y, Y=Y)
+    for rows, res in ((slice(-300, None), tail), (slice(0, 300), None), (slice(65536 - 40, 65536 + 260), None)):
+        want = sq.w4a4_linear(A_[rows].clone(), s_a[rows].clone(), Wf, s_w, bias=bias, act="relu", residual=res,
+                              dtype=dtype)
+        assert torch.equal(got[rows], want)
+    del Y, got
