@@ -84,7 +84,10 @@ struct Step {
 // never mixes scales: four lane-row exchanges per 32 codes.
 // With a fused epilogue (E) the wave that adds a tile up applies it; gated, the ups of a
 // lane's gates lie 32 lanes on in the same tile (see epilogue.hpp).
-template <int TM, int NG, int GROUP, class E>
+// XL: X is read four rows of 256 bytes an instruction, in whole lines, and takes the operands' order
+// (16 rows of 16 bytes a quarter of the wave) through 4 KB of LDS of the wave's own; without, rows are read
+// in that order, which costs the address units a line for each row and quarter.
+template <int TM, int NG, int GROUP, bool XL, class E>
 __global__ __launch_bounds__(TM == 4 ? 256 : 512) void w4a16_kernel(const uint16_t* __restrict__ X,
                                                                     const uint8_t* __restrict__ Wf,
                                                                     const uint16_t* __restrict__ s_w, int M, int N,
@@ -105,11 +108,18 @@ __global__ __launch_bounds__(TM == 4 ? 256 : 512) void w4a16_kernel(const uint16
     const __amdgpu_buffer_rsrc_t rX = make_rsrc(X + (int64_t)m0 * K, (uint32_t)min(M - m0, 16 * TM) * K * 2);
     const int s_col = scale_index<E::kGlu>(g0 + r % NG, 4 * g, N);
     const uint32_t sv = (E::kGlu ? g0 + r % NG < groups : s_col < N) ? (uint32_t)s_col * 2 : kOOB;
-    uint32_t wv[NG], xv[TM];
+    uint32_t wv[NG], xv[TM][XL ? 4 : 1];
 #pragma unroll
     for (int n = 0; n < NG; ++n) wv[n] = g0 + n < groups ? (uint32_t)(g0 + n) * 1024 + lane * 16 : kOOB;
 #pragma unroll
-    for (int i = 0; i < TM; ++i) xv[i] = m0 + 16 * i + r < M ? (uint32_t)((16 * i + r) * K + 8 * g) * 2 : kOOB;
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int q = 0; q < (XL ? 4 : 1); ++q) {
+            // XL: of load q lane (g, r) takes row 4 q + g's chunk of 8 inputs that belongs in its place of LDS (xor: the
+            // reads of a chunk of 16 rows then meet every bank once)
+            const int row = 16 * i + (XL ? 4 * q + g : r), k = 8 * (XL ? r ^ (4 * q + g) : g);
+            xv[i][q] = m0 + row < M ? (uint32_t)(row * K + k) * 2 : kOOB;
+        }
     // EDGE: the step may lie past the last one or be its half (K is a multiple of 64)
     auto fetch = [&](int t, auto edge, Step<TM, NG, CH>& f) {
         constexpr bool kEdge = decltype(edge)::value;
@@ -131,12 +141,14 @@ __global__ __launch_bounds__(TM == 4 ? 256 : 512) void w4a16_kernel(const uint16
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
                 // (an offset in the scalar part that passes the buffer would undo the check of the other)
-                const bool some = !kEdge || t * 128 + 32 * s < K;
+                const bool some = !kEdge || (XL ? t * 128 + 8 * (r ^ (4 * s + g)) < K : t * 128 + 32 * s < K);
+                const int base = XL ? (kEdge ? at : t) * 256 : some ? t * 256 + 64 * s : 0;
                 f.x[i][s] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(
-                                rX, (int)(some ? xv[i] : kOOB), some ? t * 256 + 64 * s : 0, 0));
+                                rX, (int)(some ? xv[i][XL ? s : 0] : kOOB), base, 0));
             }
     };
     const NibbleMasks masks = nibble_masks();
+    v4i* own = reinterpret_cast<v4i*>(sm) + wave * (XL ? TM * 4 * kWave : 0);
     f4 sum[NG][TM];
 #pragma unroll
     for (int n = 0; n < NG; ++n)
@@ -147,7 +159,20 @@ __global__ __launch_bounds__(TM == 4 ? 256 : 512) void w4a16_kernel(const uint16
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
-            for (int s = 0; s < 4; ++s) x[i][s] = same_order(f.x[i][s]);
+            for (int s = 0; s < 4; ++s) {
+                if constexpr (XL)
+                    own[(i * 4 + s) * kWave + lane] = f.x[i][s];
+                else
+                    x[i][s] = same_order(f.x[i][s]);
+            }
+        if constexpr (XL) {
+            asm volatile("" ::: "memory");                 // (a wave's LDS accesses stay in order)
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int s = 0; s < 4; ++s) x[i][s] = same_order(own[(16 * i + r) * 16 + ((4 * s + g) ^ r)]);
+            asm volatile("" ::: "memory");
+        }
         auto one = [&](auto index) {
             constexpr int n = decltype(index)::value;
             uint32_t c[4] = {(uint32_t)f.w[n][0], (uint32_t)f.w[n][1], (uint32_t)f.w[n][2], (uint32_t)f.w[n][3]};
@@ -215,6 +240,7 @@ __global__ __launch_bounds__(TM == 4 ? 256 : 512) void w4a16_kernel(const uint16
             bias[u] = load_b64(bB, (uint32_t)scale_index<E::kGlu>(g0 + n, 4 * g, N) * 2);
         }
     }
+    if (XL) __syncthreads();                           // the sums take the place of the waves' rows
     f4* red = reinterpret_cast<f4*>(sm);               // [wave][NG][TM][lane]
 #pragma unroll
     for (int n = 0; n < NG; ++n)
@@ -282,18 +308,20 @@ __global__ __launch_bounds__(256) void quantize_group_kernel(const uint16_t* __r
     if (lane == 0) s_w[(int64_t)gi * N + n] = sh;
 }
 
-template <int TM, int NG, class E>
+template <int TM, int NG, bool XL, class E>
 hipError_t launch_tile(const uint16_t* X, const uint8_t* Wf, const uint16_t* s_w, int M, int N, int K, int group,
                        uint16_t* Y, int waves, hipStream_t st, const E& e) {
     const dim3 grid((unsigned)(((N + 15) / 16 + NG - 1) / NG), (unsigned)((M + 16 * TM - 1) / (16 * TM)));
     const dim3 block(kWave * waves);
-    const size_t lds = (size_t)waves * NG * TM * kWave * sizeof(f4);
+    const size_t sums = (size_t)waves * NG * TM * kWave * sizeof(f4), rows = XL ? (size_t)waves * TM * 4096 : 0;
+    const size_t lds = sums > rows ? sums : rows;
+    if (lds > 64 * 1024) return hipErrorInvalidConfiguration;
     if (group == 32)
-        hipLaunchKernelGGL((w4a16_kernel<TM, NG, 32, E>), grid, block, lds, st, X, Wf, s_w, M, N, K, group, Y, e);
+        hipLaunchKernelGGL((w4a16_kernel<TM, NG, 32, XL, E>), grid, block, lds, st, X, Wf, s_w, M, N, K, group, Y, e);
     else if (group == 64)
-        hipLaunchKernelGGL((w4a16_kernel<TM, NG, 64, E>), grid, block, lds, st, X, Wf, s_w, M, N, K, group, Y, e);
+        hipLaunchKernelGGL((w4a16_kernel<TM, NG, 64, XL, E>), grid, block, lds, st, X, Wf, s_w, M, N, K, group, Y, e);
     else
-        hipLaunchKernelGGL((w4a16_kernel<TM, NG, 128, E>), grid, block, lds, st, X, Wf, s_w, M, N, K, group, Y, e);
+        hipLaunchKernelGGL((w4a16_kernel<TM, NG, 128, XL, E>), grid, block, lds, st, X, Wf, s_w, M, N, K, group, Y, e);
     return hipGetLastError();
 }
 
@@ -302,15 +330,20 @@ hipError_t launch_plan(const uint16_t* X, const uint8_t* Wf, const uint16_t* s_w
                        uint16_t* Y, hipStream_t st, const E& e) {
     const W4a16Plan p = w4a16_plan(M, N);
     switch (p.tm * 8 + p.ng) {
-        case 8 + 1: return launch_tile<1, 1>(X, Wf, s_w, M, N, K, group, Y, p.waves, st, e);
-        case 8 + 2: return launch_tile<1, 2>(X, Wf, s_w, M, N, K, group, Y, p.waves, st, e);
-        case 8 + 3: return launch_tile<1, 3>(X, Wf, s_w, M, N, K, group, Y, p.waves, st, e);
-        case 8 + 4: return launch_tile<1, 4>(X, Wf, s_w, M, N, K, group, Y, p.waves, st, e);
-        case 8 + 5: return launch_tile<1, 5>(X, Wf, s_w, M, N, K, group, Y, p.waves, st, e);
-        case 16 + 1: return launch_tile<2, 1>(X, Wf, s_w, M, N, K, group, Y, p.waves, st, e);
-        case 16 + 2: return launch_tile<2, 2>(X, Wf, s_w, M, N, K, group, Y, p.waves, st, e);
-        case 32 + 1: return launch_tile<4, 1>(X, Wf, s_w, M, N, K, group, Y, p.waves, st, e);
-        case 32 + 2: return launch_tile<4, 2>(X, Wf, s_w, M, N, K, group, Y, p.waves, st, e);
+        case 8 + 1:
+            return p.lines ? launch_tile<1, 1, true>(X, Wf, s_w, M, N, K, group, Y, p.waves, st, e) : launch_tile<1, 1, false>(X, Wf, s_w, M, N, K, group, Y, p.waves, st, e);
+        case 8 + 2:
+            return p.lines ? launch_tile<1, 2, true>(X, Wf, s_w, M, N, K, group, Y, p.waves, st, e) : launch_tile<1, 2, false>(X, Wf, s_w, M, N, K, group, Y, p.waves, st, e);
+        case 8 + 3:
+            return p.lines ? launch_tile<1, 3, true>(X, Wf, s_w, M, N, K, group, Y, p.waves, st, e) : launch_tile<1, 3, false>(X, Wf, s_w, M, N, K, group, Y, p.waves, st, e);
+        case 8 + 4:
+            return p.lines ? launch_tile<1, 4, true>(X, Wf, s_w, M, N, K, group, Y, p.waves, st, e) : launch_tile<1, 4, false>(X, Wf, s_w, M, N, K, group, Y, p.waves, st, e);
+        case 8 + 5:
+            return p.lines ? launch_tile<1, 5, true>(X, Wf, s_w, M, N, K, group, Y, p.waves, st, e) : launch_tile<1, 5, false>(X, Wf, s_w, M, N, K, group, Y, p.waves, st, e);
+        case 16 + 1: return launch_tile<2, 1, true>(X, Wf, s_w, M, N, K, group, Y, p.waves, st, e);
+        case 16 + 2: return launch_tile<2, 2, true>(X, Wf, s_w, M, N, K, group, Y, p.waves, st, e);
+        case 32 + 1: return launch_tile<4, 1, true>(X, Wf, s_w, M, N, K, group, Y, p.waves, st, e);
+        case 32 + 2: return launch_tile<4, 2, true>(X, Wf, s_w, M, N, K, group, Y, p.waves, st, e);
         default: return hipErrorInvalidConfiguration;
     }
 }

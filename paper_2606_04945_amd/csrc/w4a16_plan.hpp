@@ -17,10 +17,11 @@ namespace sq {
 
 struct W4a16Plan {
     int tm, ng, waves;     // row tiles of 16, groups of 16 outputs, waves
+    bool lines;            // X read in whole lines and reordered through LDS
 };
 
 inline W4a16Plan w4a16_plan(int M, int N) {
-    W4a16Plan p{M <= 16 ? 1 : M <= 32 ? 2 : 4, 1, 4};
+    W4a16Plan p{M <= 16 ? 1 : M <= 32 ? 2 : 4, 1, 4, M > 4};
     const int64_t groups = ((int64_t)N + 15) / 16, row_tiles = ((int64_t)M + 16 * p.tm - 1) / (16 * p.tm);
     const int64_t rows = 4 + 12 * (M < 16 * p.tm ? M : 16 * p.tm) / 16;      // in sixteenths of a group
     int64_t best = INT64_MAX;
