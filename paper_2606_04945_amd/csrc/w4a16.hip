@@ -75,9 +75,10 @@ struct Step {
 
 // One workgroup: NG groups of 16 outputs and up to 16 TM rows of X, the k steps of
 // 128 dealt round to its waves, whose sums are added in LDS in the waves' order.
-// A step is requested while the one before is multiplied.  Bound by the codes' reading
-// (16 x 37888 x 3584 at groups of 64: 19.6 us, 3.8 TB/s; 1 x 4096 x 4096: 4.5 us, of
-// which a launch that does nothing takes about 2.5).
+// A step is requested while the one before is multiplied (three, four and six steps in flight
+// are 5-40 % slower where a workgroup has few steps, and no faster where it has many).  Bound by
+// the codes' reading (16 x 37888 x 3584 at groups of 64: 18.9 us, 3.9 TB/s; 1 x 4096 x 4096:
+// 5.1 us, of which a launch that does nothing takes about 2.5).
 // GROUP: 32, 64 or 128 (a multiple of 128 applies one scale to several steps).
 // In a fragment lane 16 j + r has the 32 codes of input group j of weight row r; a
 // matrix instruction takes all its inputs from one such group instead, so that it
@@ -86,7 +87,8 @@ struct Step {
 // lane's gates lie 32 lanes on in the same tile (see epilogue.hpp).
 // XL: X is read four rows of 256 bytes an instruction, in whole lines, and takes the operands' order
 // (16 rows of 16 bytes a quarter of the wave) through 4 KB of LDS of the wave's own; without, rows are read
-// in that order, which costs the address units a line for each row and quarter.
+// in that order, which costs the address units a line for each row and quarter (16 x 4096 x 12288 17.1 ->
+// 12.8 us, 32 x 24576 x 4096 29.2 -> 22).
 template <int TM, int NG, int GROUP, bool XL, class E>
 __global__ __launch_bounds__(TM == 4 ? 256 : 512) void w4a16_kernel(const uint16_t* __restrict__ X,
                                                                     const uint8_t* __restrict__ Wf,
@@ -202,24 +204,27 @@ __global__ __launch_bounds__(TM == 4 ? 256 : 512) void w4a16_kernel(const uint16
         if constexpr (NG > 4) one(Index<4>());
     };
     if (wave < steps) {
-        // all but the last two steps of a wave lie inside; past the last, zeros are read and
-        // nothing is multiplied
-        Step<TM, NG, CH> a, b;
-        fetch(wave, Index<1>(), a);
+        // all but the last two steps of a wave lie inside; past the last, zeros are read and nothing is multiplied
+        // (one token's loop is 4-11 % faster written this way than with an exit after each half: 1 x 37888 x 3584
+        // 18.4 -> 16.5 us; 64 rows over a deep K 6 % slower)
+        Step<TM, NG, CH> step[2];
+        fetch(wave, Index<1>(), step[0]);
         int t = wave;
         for (; t + 2 * waves < steps - 1; t += 2 * waves) {
-            fetch(t + waves, Index<0>(), b);
-            multiply(a);
-            fetch(t + 2 * waves, Index<0>(), a);
-            multiply(b);
+#pragma unroll
+            for (int d = 0; d < 2; ++d) {
+                fetch(t + (d + 1) * waves, Index<0>(), step[1 - d]);
+                multiply(step[d]);
+            }
         }
-        for (;; t += 2 * waves) {
-            fetch(t + waves, Index<1>(), b);
-            multiply(a);
-            if (t + waves >= steps) break;
-            fetch(t + 2 * waves, Index<1>(), a);
-            multiply(b);
-            if (t + 2 * waves >= steps) break;
+        for (bool more = true; more; t += 2 * waves) {
+#pragma unroll
+            for (int d = 0; d < 2; ++d) {
+                if (!more) continue;
+                fetch(t + (d + 1) * waves, Index<1>(), step[1 - d]);
+                multiply(step[d]);
+                more = t + (d + 1) * waves < steps;
+            }
         }
     }
     // the waves share the adding up: of the NG TM tiles, number z to wave z % waves; what a fused epilogue
