@@ -1,3 +1,5 @@
+// Products on row-major weights and the reordering of weights; the kernels they share with the
+// fragment-ordered products, and how codes become operands, are in gemm_kernels.hpp.
 #include "gemm_kernels.hpp"
 #include "layer.hpp"
 

@@ -29,6 +29,9 @@
 //
 // BITS = 8 is the W8A8 variant (App. D): codes are int8 already, so the same
 // tiles feed the MFMA straight from LDS with no unpacking and no scaling.
+//
+// E is what is done with the sums (epilogue.hpp): dequantised as above, or with bias,
+// activation, gate and residual.
 #pragma once
 #include "epilogue.hpp"
 #include "gemm_plan.hpp"
@@ -529,7 +532,8 @@ struct ShortEpilogue {
             for (int i = 0; i < TM; ++i)
 #pragma unroll
                 for (int r = 0; r < R; ++r)
-                    res[i][r] = res_load_one(b, (uint32_t)(row(i, r, lr, lg) * NO + col), col < NO && row(i, r, lr, lg) < M);
+                    res[i][r] = res_load_one(b, (uint32_t)(row(i, r, lr, lg) * NO + col),
+                                             col < NO && row(i, r, lr, lg) < M);
         }
     }
     __device__ __forceinline__ void store(const E& f, float (&t)[TM][4], int grp, int lr, int lg, int M, int N) const {
