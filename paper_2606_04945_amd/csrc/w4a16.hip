@@ -334,23 +334,20 @@ template <class E>
 hipError_t launch_plan(const uint16_t* X, const uint8_t* Wf, const uint16_t* s_w, int M, int N, int K, int group,
                        uint16_t* Y, hipStream_t st, const E& e) {
     const W4a16Plan p = w4a16_plan(M, N);
+#define WITH(TM, NG, XL) launch_tile<TM, NG, XL>(X, Wf, s_w, M, N, K, group, Y, p.waves, st, e)
     switch (p.tm * 8 + p.ng) {
-        case 8 + 1:
-            return p.lines ? launch_tile<1, 1, true>(X, Wf, s_w, M, N, K, group, Y, p.waves, st, e) : launch_tile<1, 1, false>(X, Wf, s_w, M, N, K, group, Y, p.waves, st, e);
-        case 8 + 2:
-            return p.lines ? launch_tile<1, 2, true>(X, Wf, s_w, M, N, K, group, Y, p.waves, st, e) : launch_tile<1, 2, false>(X, Wf, s_w, M, N, K, group, Y, p.waves, st, e);
-        case 8 + 3:
-            return p.lines ? launch_tile<1, 3, true>(X, Wf, s_w, M, N, K, group, Y, p.waves, st, e) : launch_tile<1, 3, false>(X, Wf, s_w, M, N, K, group, Y, p.waves, st, e);
-        case 8 + 4:
-            return p.lines ? launch_tile<1, 4, true>(X, Wf, s_w, M, N, K, group, Y, p.waves, st, e) : launch_tile<1, 4, false>(X, Wf, s_w, M, N, K, group, Y, p.waves, st, e);
-        case 8 + 5:
-            return p.lines ? launch_tile<1, 5, true>(X, Wf, s_w, M, N, K, group, Y, p.waves, st, e) : launch_tile<1, 5, false>(X, Wf, s_w, M, N, K, group, Y, p.waves, st, e);
-        case 16 + 1: return launch_tile<2, 1, true>(X, Wf, s_w, M, N, K, group, Y, p.waves, st, e);
-        case 16 + 2: return launch_tile<2, 2, true>(X, Wf, s_w, M, N, K, group, Y, p.waves, st, e);
-        case 32 + 1: return launch_tile<4, 1, true>(X, Wf, s_w, M, N, K, group, Y, p.waves, st, e);
-        case 32 + 2: return launch_tile<4, 2, true>(X, Wf, s_w, M, N, K, group, Y, p.waves, st, e);
+        case 8 + 1: return p.lines ? WITH(1, 1, true) : WITH(1, 1, false);
+        case 8 + 2: return p.lines ? WITH(1, 2, true) : WITH(1, 2, false);
+        case 8 + 3: return p.lines ? WITH(1, 3, true) : WITH(1, 3, false);
+        case 8 + 4: return p.lines ? WITH(1, 4, true) : WITH(1, 4, false);
+        case 8 + 5: return p.lines ? WITH(1, 5, true) : WITH(1, 5, false);
+        case 16 + 1: return WITH(2, 1, true);
+        case 16 + 2: return WITH(2, 2, true);
+        case 32 + 1: return WITH(4, 1, true);
+        case 32 + 2: return WITH(4, 2, true);
         default: return hipErrorInvalidConfiguration;
     }
+#undef WITH
 }
 
 }  // namespace

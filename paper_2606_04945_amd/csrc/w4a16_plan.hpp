@@ -8,11 +8,11 @@
 //   1 x 24576 x 4096:  13.9 12.6 12.6 14.2 18.6, estimate 7.8 6.9 6.6 8.6 10.6
 //   1 x 4096 x 4096:   4.6 5.3 6.4 7.2 9.9,      estimate 1.3 2.3 3.3 4.3 5.3
 // Eight waves where workgroups are few (5 x 3584 x 18944 20.6 -> 15.1), four otherwise
-// (2 x 12288 x 4096, NG = 1: 9.5 -> 8.5; 32 x 12288 x 4096, NG = 2: 19.0 -> 16.3).  Above 16 rows the registers hold at most two
-// groups, and above 32 those of four waves.
+// (2 x 12288 x 4096, NG = 1: 9.5 -> 8.5; 32 x 12288 x 4096, NG = 2: 19.0 -> 16.3).  Above
+// 16 rows the registers hold at most two groups, and above 32 those of four waves.
 // (These figures are of rows read in the operands' order, which now only up to four rows are;
-// in whole lines and through LDS, us at 4, 8 and 16 rows: 4096 x 12288 12.9 14.3 17.1 -> 12.0 12.0 12.8, 4096 x
-// 4096 5.6 6.1 7.3 -> 5.9 6.0 6.1.)
+// in whole lines and through LDS, us at 4, 8 and 16 rows: 4096 x 12288 12.9 14.3 17.1 ->
+// 12.0 12.0 12.8, 4096 x 4096 5.6 6.1 7.3 -> 5.9 6.0 6.1.)
 #pragma once
 #include <stdint.h>
 
