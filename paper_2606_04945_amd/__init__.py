@@ -120,6 +120,9 @@ def quant_act_workspace_bytes(M: int, K: int, has_P: bool, has_tac: bool) -> int
     return int(lib().sq_quant_act_workspace_bytes(M, K, int(has_P), int(has_tac)))
 
 
+_quant_workspace_bytes = functools.lru_cache(maxsize=4096)(quant_act_workspace_bytes)      # of sizes alone
+
+
 def prepare_weights_workspace_bytes(N: int, K: int, has_P: bool) -> int:
     return int(lib().sq_prepare_weights_workspace_bytes(N, K, int(has_P)))
 
@@ -217,12 +220,14 @@ def sgat_quant_act(X: torch.Tensor, state: Optional[torch.Tensor], P: Optional[t
         _need(tac_M, "tac_M", torch.float16, (K // g, g, g))
         _need(tac_d, "tac_d", torch.float16, (K,))
     if Aq is None:
-        Aq = torch.empty((M, kw), dtype=dt, device=X.device)
+        Aq = X.new_empty((M, kw), dtype=dt)
+    else:
+        _need(Aq, "Aq", dt, (M, kw))
     if s_a is None:
-        s_a = torch.empty((M,), dtype=torch.float32, device=X.device)
-    _need(Aq, "Aq", dt, (M, kw))
-    _need(s_a, "s_a", torch.float32, (M,))
-    ws, wsb = _ws(quant_act_workspace_bytes(M, K, P is not None, tac_M is not None), ws, X.device)
+        s_a = X.new_empty((M,), dtype=torch.float32)
+    else:
+        _need(s_a, "s_a", torch.float32, (M,))
+    ws, wsb = _ws(_quant_workspace_bytes(M, K, P is not None, tac_M is not None), ws, X.device)
     f = lib().sgat_quant_act_w8 if bits == 8 else lib().sgat_quant_act
     check(f(_ptr(X), _ptr(state), _ptr(P), M, K, d_m, d_u, _ptr(tac_M), _ptr(tac_d), g,
             _ptr(Aq), _ptr(s_a), _ptr(ws), wsb, _stream(stream)))
@@ -845,7 +850,7 @@ def norm(h: torch.Tensor, y: Optional[torch.Tensor] = None, *, weight=None, post
     [seqs, K] fp16 (rows any multiple of 8 apart) of which token i takes row seq[i], or [K].  Without y
     h' is h.  Returns (X, h'); h_out may be h."""
     if out is None:
-        out = h.new_empty(h.shape, dtype=torch.float16)
+        out = torch.empty_like(h, dtype=torch.float16)
     else:
         _need(out, "out", torch.float16, h.shape)
     return out, _norm(h, y, weight, post_weight, gate, alpha, scale, shift, seq, eps, center, h_out, out, None, None, None,
