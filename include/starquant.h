@@ -552,7 +552,7 @@ int w4a16_linear(const uint16_t* X, const uint8_t* Wf, const uint16_t* s_w, int3
  * operation in the order written.  What is NULL is left out.
  *   h        [M][K] fp16, or fp32 if `f32`.        y  [M][K] fp16, the block's output.
  *   gate, scale, shift  [seqs][K] fp16 each, their rows gate_row ... elements apart (multiples
- *            of 8, at least K; of no account for one row): per-sequence conditioning, or
+ *            of 8, at least K, or 0: one row for all; of no account for one row): per-sequence conditioning, or
  *            with one row a layer's own scales and biases.
  *   seq      [M] int32 (4-byte aligned), the row of those that a token takes, clamped to 0 ..
  *            seqs - 1; NULL: row 0.

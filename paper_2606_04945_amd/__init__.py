@@ -784,8 +784,9 @@ def w4a16_linear(X: torch.Tensor, Wf: torch.Tensor, s_w: torch.Tensor, *, bias=N
 
 
 def _conditions(K: int, gate, scale, shift):
-    """(rows, distances between them) of gate, scale and shift, [seqs, K] or [K]; None: not given."""
-    seqs, strides = 0, []
+    """(rows, distances between them) of gate, scale and shift, [seqs, K], or [K] or [1, K] for all; None: not
+    given."""
+    seqs, strides = 1, []
     for t, name in ((gate, "gate"), (scale, "scale"), (shift, "shift")):
         if t is None:
             strides.append(0)
@@ -795,10 +796,10 @@ def _conditions(K: int, gate, scale, shift):
         n = t.shape[0] if t.dim() == 2 else 1
         if t.stride(-1) != 1:
             raise ValueError(f"{name} must be dense in its last dimension")
-        if n == 0 or (seqs and n != seqs):
-            raise ValueError("gate, scale and shift must have the same number of rows, at least one")
-        seqs = n
-        strides.append(t.stride(0) if t.dim() == 2 else K)
+        if n == 0 or (n > 1 and seqs > 1 and n != seqs):
+            raise ValueError("gate, scale and shift must have the same number of rows, or one")
+        seqs = max(seqs, n)
+        strides.append(t.stride(0) if n > 1 else 0)
     return seqs, strides
 
 
@@ -847,7 +848,7 @@ def norm(h: torch.Tensor, y: Optional[torch.Tensor] = None, *, weight=None, post
     """The block output y [M, K] onto the residual stream h [M, K] (fp16 or fp32), and the norm of
     the sum: h' = h + alpha gate y (y normed itself with post_weight), X = norm(h') weight (1 + scale)
     + shift, fp16.  RMS norm, or with center=True the mean taken off.  gate, scale and shift are
-    [seqs, K] fp16 (rows any multiple of 8 apart) of which token i takes row seq[i], or [K].  Without y
+    [seqs, K] fp16 (rows any multiple of 8 apart) of which token i takes row seq[i], or [K] for all tokens.  Without y
     h' is h.  Returns (X, h'); h_out may be h."""
     if out is None:
         out = torch.empty_like(h, dtype=torch.float16)

@@ -863,10 +863,10 @@ int sq_norm(const sq_norm_args* args, int32_t M, int32_t K, void* stream) {
     SQ_REQUIRE(!rows || a.seqs >= 1, SQ_ERR_SHAPE, "sq_norm: seqs=%d < 1", a.seqs);
     if (rows && a.seqs > 1) {
         auto bad = [&](const uint16_t* p, int64_t row) {
-            return p && (row < K || row % 8 || row > ((int64_t)1 << 32));
+            return p && row != 0 && (row < K || row % 8 || row > ((int64_t)1 << 32));
         };
         SQ_REQUIRE(!bad(a.gate, a.gate_row) && !bad(a.scale, a.scale_row) && !bad(a.shift, a.shift_row), SQ_ERR_SHAPE,
-                   "sq_norm: rows of gate, scale and shift must be multiples of 8 and at least K=%d apart", K);
+                   "sq_norm: rows of gate, scale and shift must be multiples of 8 and at least K=%d apart, or 0", K);
     }
     if (a.codes || a.s) {
         SQ_REQUIRE(a.bits == 4 || a.bits == 8, SQ_ERR_SHAPE, "sq_norm: bits=%d: need 4 or 8", a.bits);

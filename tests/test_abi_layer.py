@@ -112,6 +112,7 @@ def test_norm(lib):
                {**rows, "scale": BAD}, {**codes, "codes": FAR + 4}, {**codes, "s": FAR + (1 << 20) + 4}):
         assert norm(lib, **kw) == L.SQ_ERR_ALIGN, kw
     assert norm(lib, M=0, h=None) == L.SQ_OK
+    assert norm(lib, M=0, **{**rows, "scale_row": 0, "shift_row": 0}) == L.SQ_OK     # one row for all
 
 
 def test_binding_refuses():

@@ -235,3 +235,22 @@ def test_offsets_past_31_bits():
     X, _ = sq.norm(h, out=torch.empty_like(h))
     assert torch.equal(X[-3:], want) and not bool(X[:100].any())
     del X, h
+
+
+@pytest.mark.parametrize("shared", ["gate", "scale", "shift"])
+def test_one_row_among_rows_of_conditions(shared):
+    """A layer's own row with per-sequence ones, as [K], as [1, K] and as a view that repeats it."""
+    rng = np.random.default_rng(3)
+    c = Case(rng, 9, 520, gate=True, mod=True, post=True, seqs=4)
+    kw = c.device_kw(alpha=0.5)
+    row = kw[shared][1]
+    c.kw[shared] = np.repeat(c.kw[shared][1:2], 4, 0)
+    n, h = c.want(alpha=0.5)
+    for form in (row.clone(), row.clone()[None], row.clone()[None].expand(4, -1)):
+        X, h2 = sq.norm(dev(c.h), dev(c.y), **{**kw, shared: form})
+        assert_bits(host(X), n.astype(np.float16), "X")
+        assert_bits(host(h2), h, "h'")
+    with pytest.raises(ValueError):
+        sq.norm(dev(c.h), dev(c.y), **{**kw, shared: row[None].expand(3, -1)})
+    with pytest.raises(ValueError):
+        sq.norm(dev(c.h), dev(c.y), **{**kw, "seq": None})
