@@ -730,10 +730,12 @@ def _epilogue(M: int, N: int, like: torch.Tensor, bias, act: str, glu: bool, res
         _need(bias, "bias", torch.float16, (N,))
     if residual is not None:
         _need(residual, "residual", dtype, shape)
-    if Y is None:
-        Y = like.new_empty(shape, dtype=dtype)
-    else:
+    if Y is not None:
         _need(Y, "Y", dtype, shape)
+    elif residual is not None:
+        Y = torch.empty_like(residual)
+    else:
+        Y = like.new_empty(shape, dtype=dtype)
     return EPILOGUE.pack(_at(bias), _at(residual), _choice(ACTIVATIONS, act, "act"), bool(glu), f32), Y
 
 
