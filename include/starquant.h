@@ -560,7 +560,7 @@ int w4a16_linear(const uint16_t* X, const uint8_t* Wf, const uint16_t* s_w, int3
  *   h_out    [M][K] of h's type; may be h.  X [M][K] fp16.
  *   codes, s [M][K / 2] packed int4 (bits = 4) or [M][K] int8 (bits = 8) and [M] fp32, both
  *            or neither; state, d_m, d_u as in sgat_quant_act.  A row that holds (or makes) a NaN
- *            or an infinity has scale NaN and zero codes.
+ *            or an infinity, in a band that its state drops too, has scale NaN and zero codes.
  *   At least one of h_out, X and codes.  Outputs overlap nothing else.
  *   K % 8 == 0, 8 <= K <= 32768; with codes K % 64 == 0.  M <= 4194240.
  */

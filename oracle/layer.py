@@ -196,3 +196,12 @@ def quantise(n, bits):
     s = s.copy()
     s[bad] = np.nan
     return q, s
+
+
+def quantise_gated(n, state, dm, du, bits):
+    """The same of gated rows; what a state drops counts for whether a row is finite."""
+    q, s = quantise(gated(n, state, dm, du), bits)
+    bad = ~np.isfinite(n).all(1)
+    q, s = q.copy(), s.copy()
+    q[bad], s[bad] = 0, np.nan
+    return q, s

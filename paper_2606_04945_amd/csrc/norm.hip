@@ -292,7 +292,11 @@ __global__ __launch_bounds__(kWave * (WAVES == 1 ? kRowsPerGroup : WAVES)) void 
     statistics([&](int i, float (&x)[8]) { h[i].get(x); }, mean, rate);
     // the gate keeps columns [0, lim0) and [lim1, K)
     const int lim0 = a.state ? (masked ? K - a.d_u : K - a.d_m - a.d_u) : K, lim1 = masked ? K : K - a.d_u;
-    float n[NV][8], most = 0.0f;
+    float n[NV][8], most = 0.0f, lost = 0.0f;          // largest entry kept, and dropped
+    auto drop = [&](const float (&x)[8]) {
+#pragma unroll
+        for (int q = 0; q < 8; ++q) lost = __builtin_elementwise_maximum(lost, fabsf(x[q]));
+    };
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int v = t + i * lanes;
@@ -318,12 +322,15 @@ __global__ __launch_bounds__(kWave * (WAVES == 1 ? kRowsPerGroup : WAVES)) void 
         }
         if (a.X && v * 8 < K) *reinterpret_cast<v4i*>(a.X + at + v * 8) = to_halves(x);
         if (BITS == 0) continue;
-        // nearly every vector is kept or dropped whole (a masked row drops its u-band, an unmasked one its m-band)
+        // nearly every vector is kept or dropped whole (a masked row drops its u-band, an unmasked one its m-band);
+        // past the row an entry is what the mean makes of a zero, and no part of it
         const int c = 8 * v;
         if ((c >= K) | ((c >= lim0) & (c + 8 <= lim1))) {
+            if (c < K) drop(x);
 #pragma unroll
             for (int q = 0; q < 8; ++q) x[q] = 0.0f;
         } else if ((c + 8 > lim0) & (c < lim1)) {
+            drop(x);
 #pragma unroll
             for (int q = 0; q < 8; ++q) x[q] = (c + q < lim0) | (c + q >= lim1) ? x[q] : 0.0f;
         }
@@ -332,8 +339,9 @@ __global__ __launch_bounds__(kWave * (WAVES == 1 ? kRowsPerGroup : WAVES)) void 
     }
     if constexpr (BITS != 0) {
         constexpr int QMAX = BITS == 4 ? 7 : 127;
-        most = group.most(most);
-        // a row with an entry that is not finite: scale NaN, zero codes
+        // a row with an entry that is not finite, be it in a dropped band: scale NaN, zero codes (an infinity
+        // there has made the rate and so every kept entry of an RMS norm 0)
+        most = group.most(lost < __builtin_inff() ? most : __builtin_nanf(""));
         const float s = most < __builtin_inff() ? most / (float)QMAX : __builtin_nanf("");
         const float inv = s > 0.0f ? 1.0f / s : 0.0f;
         if (t == 0) a.s[row] = s;
