@@ -89,12 +89,30 @@ struct Step {
 // (16 rows of 16 bytes a quarter of the wave) through 4 KB of LDS of the wave's own; without, rows are read
 // in that order, which costs the address units a line for each row and quarter (16 x 4096 x 12288 17.1 ->
 // 12.8 us, 32 x 24576 x 4096 29.2 -> 22).
+//
+// How a wave's last steps end: by a flag that is looked at behind each step, or by leaving the loop (kLeave).  The
+// flag gives longer stretches of code, in which more is requested ahead, and takes more registers, so it loses
+// where they decide how many workgroups a CU holds.  Flag / leaving, us: 1 x 37888 x 3584 in groups of 64 16.5 / 18.4,
+// 1 x 4096 x 12288 of 64 10.9 / 11.9, 1 x 16384 x 4096 of 32 12.1 / 17.1, 1 x 3584 x 18944 of 32 16.9 / 17.3, but
+// 1 x 24576 x 4096 of 32 20.9 / 15.5, 1 x 12288 x 4096 of 32 11.9 / 9.9, 5 x 3584 x 18944 of 32 18.3 / 17.1, 17 x
+// 24576 x 4096 of 32 24.3 / 22.3, 16 x 24576 x 4096 of 64 18.3 / 15.9, 200 x 24576 x 4096 of 32 185 / 144.
+constexpr bool leaves(int tm, int ng, int group, bool lines) {
+    if (group > 32) return ng == 3 && lines;
+    return tm > 1 || !(ng == 4 || (ng == 1 && !lines));
+}
+// Waves of a SIMD that the registers have to leave room for, where it is more than one workgroup's: two workgroups
+// of eight waves (three groups of outputs: 5 x 24576 x 4096 of 32 19.6 -> 16.7 us, gated 1 x 24576 x 4096 of 128 15.3 ->
+// 13.9), two of four (33 rows and more, with four scales a step: 64 x 24576 x 4096 of 32 58 -> 47 us, and 44 with
+// kTile below).
+constexpr int least_waves(int tm, int ng, int group) {
+    if (tm == 4) return group == 32 ? 2 : 1;
+    return ng == 3 ? 4 : 2;
+}
 template <int TM, int NG, int GROUP, bool XL, class E>
-__global__ __launch_bounds__(TM == 4 ? 256 : 512) void w4a16_kernel(const uint16_t* __restrict__ X,
-                                                                    const uint8_t* __restrict__ Wf,
-                                                                    const uint16_t* __restrict__ s_w, int M, int N,
-                                                                    int K, int group, uint16_t* __restrict__ Y,
-                                                                    E fused) {
+__global__ __launch_bounds__(TM == 4 ? 256 : 512)
+__attribute__((amdgpu_waves_per_eu(least_waves(TM, NG, GROUP)))) void w4a16_kernel(
+    const uint16_t* __restrict__ X, const uint8_t* __restrict__ Wf, const uint16_t* __restrict__ s_w, int M, int N, int K,
+    int group, uint16_t* __restrict__ Y, E fused) {
     extern __shared__ __attribute__((aligned(16))) uint8_t sm[];
     constexpr int CH = 128 / GROUP, PER = 4 / CH;      // scales a step, matrix instructions a scale
     const int waves = blockDim.x / kWave;
@@ -110,17 +128,20 @@ __global__ __launch_bounds__(TM == 4 ? 256 : 512) void w4a16_kernel(const uint16
     const __amdgpu_buffer_rsrc_t rX = make_rsrc(X + (int64_t)m0 * K, (uint32_t)min(M - m0, 16 * TM) * K * 2);
     const int s_col = scale_index<E::kGlu>(g0 + r % NG, 4 * g, N);
     const uint32_t sv = (E::kGlu ? g0 + r % NG < groups : s_col < N) ? (uint32_t)s_col * 2 : kOOB;
-    uint32_t wv[NG], xv[TM][XL ? 4 : 1];
+    // (kTile: the offset of a row tile is added at each load, rows past M past the buffer's end by themselves)
+    constexpr bool kTile = TM == 4 && GROUP == 32;
+    constexpr int XT = kTile ? 1 : TM;
+    uint32_t wv[NG], xv[XT][XL ? 4 : 1];
 #pragma unroll
     for (int n = 0; n < NG; ++n) wv[n] = g0 + n < groups ? (uint32_t)(g0 + n) * 1024 + lane * 16 : kOOB;
 #pragma unroll
-    for (int i = 0; i < TM; ++i)
+    for (int i = 0; i < XT; ++i)
 #pragma unroll
         for (int q = 0; q < (XL ? 4 : 1); ++q) {
             // XL: of load q lane (g, r) takes row 4 q + g's chunk of 8 inputs that belongs in its place of LDS (xor: the
             // reads of a chunk of 16 rows then meet every bank once)
             const int row = 16 * i + (XL ? 4 * q + g : r), k = 8 * (XL ? r ^ (4 * q + g) : g);
-            xv[i][q] = m0 + row < M ? (uint32_t)(row * K + k) * 2 : kOOB;
+            xv[i][q] = kTile || m0 + row < M ? (uint32_t)(row * K + k) * 2 : kOOB;
         }
     // EDGE: the step may lie past the last one or be its half (K is a multiple of 64)
     auto fetch = [&](int t, auto edge, Step<TM, NG, CH>& f) {
@@ -139,15 +160,18 @@ __global__ __launch_bounds__(TM == 4 ? 256 : 512) void w4a16_kernel(const uint16
                                                                                    (int)((uint32_t)sg * N * 2), 0));
         }
 #pragma unroll
-        for (int i = 0; i < TM; ++i)
+        for (int i = 0; i < TM; ++i) {
+            uint32_t tile = kTile ? (uint32_t)(16 * i * K) * 2 : 0u;
+            if (kTile) asm volatile("" : "+s"(tile));      // (or the sums are kept in registers)
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
                 // (an offset in the scalar part that passes the buffer would undo the check of the other)
                 const bool some = !kEdge || (XL ? t * 128 + 8 * (r ^ (4 * s + g)) < K : t * 128 + 32 * s < K);
                 const int base = XL ? (kEdge ? at : t) * 256 : some ? t * 256 + 64 * s : 0;
                 f.x[i][s] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(
-                                rX, (int)(some ? xv[i][XL ? s : 0] : kOOB), base, 0));
+                                rX, (int)(some ? xv[i % XT][XL ? s : 0] + tile : kOOB), base, 0));
             }
+        }
     };
     const NibbleMasks masks = nibble_masks();
     v4i* own = reinterpret_cast<v4i*>(sm) + wave * (XL ? TM * 4 * kWave : 0);
@@ -205,8 +229,6 @@ __global__ __launch_bounds__(TM == 4 ? 256 : 512) void w4a16_kernel(const uint16
     };
     if (wave < steps) {
         // all but the last two steps of a wave lie inside; past the last, zeros are read and nothing is multiplied
-        // (one token's loop is 4-11 % faster written this way than with an exit after each half: 1 x 37888 x 3584
-        // 18.4 -> 16.5 us; 64 rows over a deep K 6 % slower)
         Step<TM, NG, CH> step[2];
         fetch(wave, Index<1>(), step[0]);
         int t = wave;
@@ -217,13 +239,24 @@ __global__ __launch_bounds__(TM == 4 ? 256 : 512) void w4a16_kernel(const uint16
                 multiply(step[d]);
             }
         }
-        for (bool more = true; more; t += 2 * waves) {
+        if constexpr (leaves(TM, NG, GROUP, XL)) {
+            for (;; t += 2 * waves) {
+                fetch(t + waves, Index<1>(), step[1]);
+                multiply(step[0]);
+                if (t + waves >= steps) break;
+                fetch(t + 2 * waves, Index<1>(), step[0]);
+                multiply(step[1]);
+                if (t + 2 * waves >= steps) break;
+            }
+        } else {
+            for (bool more = true; more; t += 2 * waves) {
 #pragma unroll
-            for (int d = 0; d < 2; ++d) {
-                if (!more) continue;
-                fetch(t + (d + 1) * waves, Index<1>(), step[1 - d]);
-                multiply(step[d]);
-                more = t + (d + 1) * waves < steps;
+                for (int d = 0; d < 2; ++d) {
+                    if (!more) continue;
+                    fetch(t + (d + 1) * waves, Index<1>(), step[1 - d]);
+                    multiply(step[d]);
+                    more = t + (d + 1) * waves < steps;
+                }
             }
         }
     }
