@@ -88,9 +88,9 @@ struct Step {
 // XL: X is read four rows of 256 bytes an instruction, in whole lines, and takes the operands' order
 // (16 rows of 16 bytes a quarter of the wave) through 4 KB of LDS of the wave's own; without, rows are read
 // in that order, which costs the address units a line for each row and quarter (16 x 4096 x 12288 17.1 ->
-// 12.8 us, 32 x 24576 x 4096 29.2 -> 22).
+// 12.8 us, 32 x 24576 x 4096 29.2 -> 22; w4a16_lines has the rule).
 //
-// How a wave's last steps end: by a flag that is looked at behind each step, or by leaving the loop (kLeave).  The
+// How a wave's last steps end: by a flag that is looked at behind each step, or by leaving the loop.  The
 // flag gives longer stretches of code, in which more is requested ahead, and takes more registers, so it loses
 // where they decide how many workgroups a CU holds.  Flag / leaving, us: 1 x 37888 x 3584 in groups of 64 16.5 / 18.4,
 // 1 x 4096 x 12288 of 64 10.9 / 11.9, 1 x 16384 x 4096 of 32 12.1 / 17.1, 1 x 3584 x 18944 of 32 16.9 / 17.3, but
@@ -366,7 +366,7 @@ hipError_t launch_tile(const uint16_t* X, const uint8_t* Wf, const uint16_t* s_w
 template <class E>
 hipError_t launch_plan(const uint16_t* X, const uint8_t* Wf, const uint16_t* s_w, int M, int N, int K, int group,
                        uint16_t* Y, hipStream_t st, const E& e) {
-    const W4a16Plan p = w4a16_plan(M, N);
+    const W4a16Plan p = w4a16_plan(M, N, K, group);
 #define WITH(TM, NG, XL) launch_tile<TM, NG, XL>(X, Wf, s_w, M, N, K, group, Y, p.waves, st, e)
     switch (p.tm * 8 + p.ng) {
         case 8 + 1: return p.lines ? WITH(1, 1, true) : WITH(1, 1, false);
