@@ -6,9 +6,13 @@
 //
 // Sums are in fp64 (an entry costs one conversion and one fused multiply-add at the fp32
 // rate, which the memory traffic hides) and the mean and r are rounded once to fp32, so
-// neither depends on the order of the sum but where a rounding border lies within
-// 2^-50 of it; every further step is one fp32 operation.  So the codes, which move where a
-// value crosses a border, do not depend on how a row is shared out.
+// neither depends on the order of the sum but where a border of fp32's rounding lies within the sum's own
+// error; every further step is one fp32 operation.  So the codes, which move where a
+// value crosses a border, do not depend on how a row is shared out.  That error: an entry goes through at most
+// 32 steps of a lane, 6 of a wave and 15 between waves, each 2^-53, so two orders differ by at most 106 2^-53 < 2^-46
+// of a sum of squares; a mean by that much of the mean magnitude, r(x) by half of it where nothing is
+// taken off.  With a mean taken off in one pass (see `statistics`) mean(x^2) is up to 17 times the variance and
+// mean^2 errs twice, so r by 25 times that, 2^-42.
 //
 // A row is held in registers by one wave or by all waves of a workgroup: it is read once,
 // every load of it in flight before the first sum.
@@ -200,8 +204,8 @@ __global__ __launch_bounds__(kWave * (WAVES == 1 ? kRowsPerGroup : WAVES)) void 
     const bool masked = BITS != 0 && a.state && a.state[row] != 0;
 
     // Mean (or 0) and r of a row whose vector i is get(i, x); its entries past K are zeros.  With a
-    // mean: both sums in one pass, mean(x^2) - mean^2 where that loses no more than four bits, else the sum of
-    // (x - mean)^2 in another.
+    // mean: both sums in one pass, mean(x^2) - mean^2 where that loses less than five bits (the difference is at
+    // least a 17th of mean(x^2)), else the sum of (x - mean)^2 in another.
     auto statistics = [&](auto get, float& mean, float& rate) {
         double s = 0.0, squares = 0.0;
 #pragma unroll
